@@ -1,0 +1,606 @@
+"""The operators of an 8-bit branch-cached MoE layer, as timed cases.
+
+What is held in 8 bits is e4m3 with one power-of-two scale for each block of
+128: a row has a scale for every 128 of its elements, a weight matrix one for
+every 128 x 128 block.  The scale of a block is 2^e with e the smallest integer
+(not below -127) for which the block's largest magnitude is at most 448 2^e;
+an element is the e4m3 number nearest to v 2^-e, ties to even.  Rows are
+padded with zeros to whole blocks and their scales (one byte each, e + 127) to
+16 bytes, which is the layout that the states below hold.
+
+* ``write``: rows are quantised as they go into slots of a cache; a slot of
+  -1 leaves its row out.  The norm of the stored row comes with it.
+* ``read``: slots of such a cache are read back in the activation type.
+* ``linear``: y = x W^T + bias; x is quantised by the call, W beforehand.
+* ``experts``: one uncached routed layer with 8-bit expert weights: router,
+  top-k gates, x quantised, up projection, activation, quantised, down
+  projection, gate-weighted sum.
+* ``cycle``: a refresh cycle of the branch-cached layer with an 8-bit cache
+  (branch rows and attention features): a full step, then steps that
+  recompute only the branches whose expert is not in the token's cache (a base
+  threshold above any score), each with its own input.
+
+Sizes are those of the DiT-MoE layers that the other cases and the tests of
+this repository use, and their neighbourhood.
+"""
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+BLOCK = 128
+TAU0, ALPHA = 8.0, 0.6  # thresholds of at least 3.2: scores end at 3
+
+
+# ---------------------------------------------------------------------------
+# cases
+# ---------------------------------------------------------------------------
+def _rows(name, kind, rows, slots, width, dtype="bf16", stride=0):
+    return {"name": name, "kind": kind, "rows": rows, "slots": slots, "width": width,
+            "dtype": dtype, "stride": stride}
+
+
+def _linear(name, M, K, N, dtype="bf16", bias=True):
+    return {"name": name, "kind": "linear", "M": M, "K": K, "N": N, "dtype": dtype, "bias": bias}
+
+
+def _layer(name, kind, d, E, k, d_ff, B, N, act="gelu_tanh", n_shared=0, steps=1, eight=True):
+    return {"name": name, "kind": kind, "d": d, "E": E, "k": k, "d_ff": d_ff, "B": B, "N": N,
+            "act": act, "n_shared": n_shared, "steps": steps, "eight": eight}
+
+
+def listed():
+    return [
+        # one image's branch rows of a cache step go into their slots: latency
+        _rows("write_154", "write", 154, 512, 1152),
+        # a full step's rows of eight images at a 64 x 64 latent
+        _rows("write_16384", "write", 16384, 16384, 1152),
+        # an fp32 layer of a width that ends inside a block, rows strided
+        _rows("write_fp32_2500", "write", 2500, 4096, 1000, dtype="fp32", stride=1100),
+        # the attention features of a few synchronised tokens are read back
+        _rows("read_300", "read", 300, 2048, 1152),
+        # every row of a batch's cache is read back
+        _rows("read_16384", "read", 16384, 16384, 1152),
+        # a single token through a projection: the weights are streamed once
+        _linear("linear_1", 1, 1152, 4608),
+        # a ragged batch of tokens, fp32 in and out, ends inside tiles and blocks
+        _linear("linear_fp32_333", 333, 1000, 1730, dtype="fp32"),
+        # a large projection, whole batch: the matrix rate
+        _linear("linear_16384", 16384, 4608, 4608),
+        # one image, 32 rows an expert: the weights of every expert are streamed
+        _layer("experts_256x1", "experts", 1152, 16, 2, 4608, 1, 256),
+        # fine-grained gated experts with shared ones: the largest call
+        _layer("experts_fine_4096x4", "experts", 2048, 64, 8, 1408, 4, 4096, act="swiglu",
+               n_shared=2),
+        # a refresh cycle at the benchmarked layer's size
+        _layer("cycle_1024x8", "cycle", 1152, 16, 2, 4608, 8, 1024, steps=4),
+        # the 8-bit cache with experts in bf16, a ragged token count, erf GELU
+        _layer("cycle_bf16_333x2", "cycle", 1152, 16, 2, 4608, 2, 333, act="gelu_erf", steps=4,
+               eight=False),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["write", "read", "linear", "linear", "linear", "experts", "experts",
+                       "cycle", "cycle"])
+    if kind in ("write", "read"):
+        rows, width = _log_int(rng, 1, 16384), _log_int(rng, 64, 4608)
+        rows = max(1, min(rows, (24 << 20) // width))
+        slots = rows + rng.randint(0, rows) if rng.random() < 0.7 else rows
+        stride = width + rng.randint(1, 300) if rng.random() < 0.4 else 0
+        c = _rows("", kind, rows, slots, width, rng.choice(["bf16", "bf16", "fp32"]), stride)
+    elif kind == "linear":
+        K, N = _log_int(rng, 64, 6144), _log_int(rng, 64, 6144)
+        M = min(_log_int(rng, 1, 16384), max(1, int(16384 * 4608 * 4608 / (K * N))))
+        c = _linear("", M, K, N, rng.choice(["bf16", "bf16", "fp32"]), rng.random() < 0.6)
+    else:
+        act = rng.choice(["gelu_tanh", "gelu_tanh", "gelu_erf", "swiglu"])
+        d, d_ff = 64 * rng.randint(4, 32), 64 * rng.randint(6, 80)
+        E = rng.choice([4, 8, 16, 24, 32, 64])
+        k = rng.choice([1, 2, 2, 3, 4])
+        shared = rng.choice([0, 0, 1, 2])
+        up = 2 if act == "swiglu" else 1
+        most = (1.3e12 if kind == "experts" else 0.8e12) / (2 * (k + shared) * d * d_ff * (up + 1))
+        T = min(_log_int(rng, 1, 16384), most)
+        B = rng.randint(1, 8)
+        N = max(1, int(T / B))
+        if kind == "cycle":
+            c = _layer("", kind, d, E, k, d_ff, B, N, act, shared, rng.choice([2, 3, 4]),
+                       rng.random() < 0.7)
+        else:
+            c = _layer("", kind, d, E, k, d_ff, B, N, act, shared)
+    del c["name"]
+    return c
+
+
+def _up_rows(c):
+    return c["d_ff"] * (2 if c["act"] == "swiglu" else 1)
+
+
+def work(case):
+    c = case
+    if c["kind"] in ("write", "read"):
+        size = 2 if c["dtype"] == "bf16" else 4
+        blocks = -(-c["width"] // BLOCK)
+        kept = int(0.9 * c["rows"]) if c["kind"] == "write" else c["rows"]
+        each = c["width"] * (size + 1) + blocks + 4
+        return {"bytes": kept * (each + (4 if c["kind"] == "write" else 0)),
+                "flops": kept * c["width"] * (4 if c["kind"] == "write" else 1)}
+    if c["kind"] == "linear":
+        size = 2 if c["dtype"] == "bf16" else 4
+        M, K, N = c["M"], c["K"], c["N"]
+        return {"bytes": size * (M * K + M * N) + N * K + -(-N // BLOCK) * -(-K // BLOCK) +
+                (4 * N if c["bias"] else 0), "flops": 2 * M * K * N}
+    T, d, E, k, S = c["B"] * c["N"], c["d"], c["E"], c["k"], c["n_shared"]
+    weights = (d * _up_rows(c) + d * c["d_ff"])  # of one expert: elements, and multiplications
+    wbytes = weights * (1 if c["eight"] else 2)
+
+    def step(rows):
+        read = min(E, rows) + S
+        return {"bytes": read * wbytes + 2 * E * d + 4 * T * d,
+                "flops": 2 * (rows + S * T) * weights + 2 * T * E * d}
+
+    full = step(T * k)
+    if c["kind"] == "experts":
+        return full
+    later = step(max(1, int(0.1 * T * k)))  # few branches lose their expert from step to step
+    n = c["steps"]
+    return {"bytes": full["bytes"] + (n - 1) * (later["bytes"] + T * k * d) + T * k * d +
+            2 * n * T * d, "flops": full["flops"] + (n - 1) * later["flops"]}
+
+
+# ---------------------------------------------------------------------------
+# inputs: the same whatever computes on them
+# ---------------------------------------------------------------------------
+def _dt(name):
+    return torch.float32 if name == "fp32" else torch.bfloat16
+
+
+def _pad(n, to):
+    return -(-n // to) * to
+
+
+def _exponents(top):
+    """e of each block from its largest magnitude."""
+    m, x = torch.frexp(top)
+    e = x - 9 + (m > 0.875).to(x.dtype)
+    return torch.where(top > 0, e, torch.full_like(e, -127)).clamp(min=-127)
+
+
+def _quant_matrix(w):
+    """Weights [n][N][K] to the stored form: bytes [n][N][pitch], scales [n][blocks][pitch]."""
+    n, N, K = w.shape
+    Kp, Np = _pad(K, BLOCK), _pad(N, BLOCK)
+    q = torch.zeros(n, N, Kp, dtype=torch.float8_e4m3fn, device=w.device)
+    s = torch.zeros(n, Np // BLOCK, _pad(Kp // BLOCK, 16), dtype=torch.uint8, device=w.device)
+    for i in range(n):
+        v = torch.zeros(Np, Kp, device=w.device)
+        v[:N, :K] = w[i].float()
+        b = v.view(Np // BLOCK, BLOCK, Kp // BLOCK, BLOCK)
+        e = _exponents(b.abs().amax((1, 3)))
+        scaled = b * torch.exp2(-e.float())[:, None, :, None]
+        q[i] = scaled.view(Np, Kp)[:N].to(torch.float8_e4m3fn)
+        s[i, :, :Kp // BLOCK] = (e + 127).to(torch.uint8)
+    return {"q": q, "s": s, "N": N, "K": K}
+
+
+class _Draws:
+    def __init__(self, seed):
+        self.g = torch.Generator(device=DEV)
+        self.g.manual_seed(seed)
+
+    def normal(self, *shape, scale=1.0):
+        return torch.randn(*shape, generator=self.g, device=DEV) * scale
+
+    def weights(self, n, N, K):
+        w = torch.empty(n, N, K, dtype=torch.bfloat16, device=DEV)
+        for i in range(n):
+            w[i] = self.normal(N, K, scale=1.0 / math.sqrt(K))
+        return w
+
+    def rows(self, rows, width, dtype, stride=0):
+        """Activations: rows of different size, a few large elements."""
+        x = self.normal(rows, stride or width) * torch.exp(self.normal(rows, 1))
+        far = torch.rand(x.shape, generator=self.g, device=DEV) < 0.002
+        return torch.where(far, x * 20, x).to(dtype)[:, :width]
+
+
+def prepare(case, seed):
+    c, g = case, _Draws(seed)
+    s = {"case": c}
+    if c["kind"] in ("write", "read"):
+        slot = torch.randperm(c["slots"], generator=g.g, device=DEV)[:c["rows"]].to(torch.int32)
+        Kp = _pad(c["width"], BLOCK)
+        Sp = _pad(Kp // BLOCK, 16)
+        if c["kind"] == "write":
+            out = torch.rand(c["rows"], generator=g.g, device=DEV) < 0.1
+            s["slot"] = torch.where(out, torch.full_like(slot, -1), slot)
+            s["x"] = g.rows(c["rows"], c["width"], _dt(c["dtype"]), c["stride"])
+            s["q"] = torch.zeros(c["slots"], Kp, dtype=torch.uint8, device=DEV)
+            s["s"] = torch.zeros(c["slots"], Sp, dtype=torch.uint8, device=DEV)
+            s["norm"] = torch.zeros(c["slots"], device=DEV)
+        else:
+            v = torch.zeros(c["slots"], Kp, device=DEV)
+            v[:, :c["width"]] = g.rows(c["slots"], c["width"], torch.float32)
+            b = v.view(c["slots"], Kp // BLOCK, BLOCK)
+            e = _exponents(b.abs().amax(2))
+            q = (b * torch.exp2(-e.float())[:, :, None]).to(torch.float8_e4m3fn)
+            s["q"] = q.view(c["slots"], Kp).view(torch.uint8)
+            s["s"] = torch.zeros(c["slots"], Sp, dtype=torch.uint8, device=DEV)
+            s["s"][:, :Kp // BLOCK] = (e + 127).to(torch.uint8)
+            s["slot"] = slot
+            s["out"] = torch.empty(c["rows"], c["stride"] or c["width"], dtype=_dt(c["dtype"]),
+                                   device=DEV)[:, :c["width"]]
+            s["norm"] = None
+        if own:
+            from paper_2606_15615_amd import quant
+            s["cache"] = quant.QuantRows(c["slots"], c["width"], q=s["q"], scale=s["s"],
+                                         norm=s["norm"])
+        return s
+    if c["kind"] == "linear":
+        s["x"] = g.rows(c["M"], c["K"], _dt(c["dtype"]))
+        w = g.weights(1, c["N"], c["K"])
+        s["w"] = _quant_matrix(w)
+        s["bias"] = g.normal(c["N"], scale=0.1) if c["bias"] else None
+        s["out"] = torch.empty(c["M"], c["N"], dtype=_dt(c["dtype"]), device=DEV)
+        if own:
+            from paper_2606_15615_amd import quant
+            s["W"] = quant.QuantMatrix(s["w"]["q"][0], s["w"]["s"][0], c["N"], c["K"])
+            s["ws"] = quant.linear_workspace(c["M"], c["K"], DEV)
+        return s
+    d, E, T = c["d"], c["E"], c["B"] * c["N"]
+    s["W_r"] = g.weights(1, E, d)[0]
+    up, down = g.weights(E, _up_rows(c), d), g.weights(E, d, c["d_ff"])
+    if c["n_shared"]:
+        up_s, down_s = g.weights(c["n_shared"], _up_rows(c), d), g.weights(c["n_shared"], d, c["d_ff"])
+    if c["eight"]:
+        s["up"], s["down"] = _quant_matrix(up), _quant_matrix(down)
+        if c["n_shared"]:
+            s["up_s"], s["down_s"] = _quant_matrix(up_s), _quant_matrix(down_s)
+    else:
+        s["up"], s["down"] = up, down
+        if c["n_shared"]:
+            s["up_s"], s["down_s"] = up_s, down_s
+    # consecutive steps of a sampling loop: every token drifts at its own rate
+    lo, hi = math.log(1e-3), math.log(2e-2)
+    a = torch.exp(lo + (hi - lo) * torch.rand(T, 1, generator=g.g, device=DEV))
+    s["x"], s["attn"] = [], []
+    for key in ("x", "attn"):
+        x = g.normal(T, d)
+        for t in range(c["steps"]):
+            if t:
+                x = torch.sqrt(1.0 - a) * x + torch.sqrt(a) * g.normal(T, d)
+            s[key].append(x.to(torch.bfloat16).view(c["B"], c["N"], d))
+    s["y"] = [torch.empty_like(x) for x in s["x"]]
+    if own:
+        s["layer"] = _make_layer(c, s)
+    return s
+
+
+def _make_layer(c, s):
+    from paper_2606_15615_amd import _lib, quant
+    from paper_2606_15615_amd.layer import MoecaLayer
+    cached = c["kind"] == "cycle"
+    L = MoecaLayer(c["d"], c["E"], c["k"], c["d_ff"], batch=c["B"], tokens=c["N"],
+                   mode=_lib.MOECA_MODE_THRESHOLD if cached else _lib.MOECA_MODE_FULL,
+                   tau0=TAU0, alpha=ALPHA, act=c["act"], n_shared=c["n_shared"], device=DEV,
+                   experts="e4m3" if c["eight"] else None, cache="e4m3" if cached else None)
+
+    def mats(w):
+        return quant.QuantMatrix(w["q"], w["s"], w["N"], w["K"])
+
+    if c["eight"]:
+        L.set_weights_quant(s["W_r"], None, mats(s["up"]), mats(s["down"]))
+        if c["n_shared"]:
+            L.set_shared_quant(mats(s["up_s"]), mats(s["down_s"]))
+    else:
+        L.set_weights(s["W_r"], None, s["up"], s["down"])
+        if c["n_shared"]:
+            L.set_shared(s["up_s"], s["down_s"])
+    if cached:
+        s["attention"] = quant.QuantRows(c["B"] * c["N"], c["d"], device=DEV)
+    return L
+
+
+# ---------------------------------------------------------------------------
+# the calls
+# ---------------------------------------------------------------------------
+def _stored(q, s, width):
+    """What 8-bit rows stand for, as they are held: elements and scales."""
+    return {"elements": q.view(torch.float8_e4m3fn)[..., :width],
+            "scales": s.view(torch.float8_e8m0fnu)[..., :-(-width // BLOCK)]}
+
+
+def _run_own(s):
+    c = s["case"]
+    if c["kind"] == "write":
+        s["cache"].write(s["x"], s["slot"])
+        return {**_stored(s["q"], s["s"], c["width"]), "norm": s["norm"]}
+    if c["kind"] == "read":
+        return s["cache"].read(s["slot"], out=s["out"])
+    if c["kind"] == "linear":
+        from paper_2606_15615_amd import quant
+        return quant.linear(s["x"], s["W"], s["bias"], out=s["out"], workspace=s["ws"])
+    L = s["layer"]
+    if c["kind"] == "experts":
+        L.step(s["x"][0], 0, s["y"][0])
+        return s["y"][0]
+    L.reset()
+    for t, x in enumerate(s["x"]):
+        L.bind_attention(s["attn"][t], s["attention"])
+        L.step(x, t, s["y"][t])
+    rows, att = L.cache_rows(), s["attention"]
+    return {"y": s["y"], "cache": _stored(rows.q, rows.scale, c["d"]),
+            "attention": _stored(att.q, att.scale, c["d"])}
+
+
+# ---- plain form: 32 bits, elementary operations ------------------------------
+def _quant(x):
+    """Rows [.., K] (fp32): elements [.., blocks, 128] and e [.., blocks]."""
+    K = x.shape[-1]
+    v = torch.nn.functional.pad(x, (0, _pad(K, BLOCK) - K))
+    b = v.view(*x.shape[:-1], v.shape[-1] // BLOCK, BLOCK)
+    e = _exponents(b.abs().amax(-1))
+    return (b * torch.exp2(-e.float())[..., None]).to(torch.float8_e4m3fn), e
+
+
+def _value(q, e, K):
+    return (q.float() * torch.exp2(e.float())[..., None]).flatten(-2)[..., :K]
+
+
+def _round_trip(x):
+    return _value(*_quant(x), x.shape[-1])
+
+
+def _held(q, s, K):
+    """The values of stored 8-bit rows."""
+    b = q.view(torch.float8_e4m3fn).float().view(q.shape[0], -1, BLOCK)
+    return _value(b, s[:, :b.shape[1]].int() - 127, K)
+
+
+def _weight(w, i=0):
+    e = w["s"][i, :, :w["q"].shape[2] // BLOCK].int() - 127
+    e = e.repeat_interleave(BLOCK, 0)[:w["N"]]
+    return _value(w["q"][i].float().view(w["N"], -1, BLOCK), e, w["K"])
+
+
+def _activation(z, act):
+    if act == "swiglu":
+        gate, up = z[:, 0::2], z[:, 1::2]
+        return gate / (1 + torch.exp(-gate)) * up
+    if act == "gelu_erf":
+        return 0.5 * z * (1 + torch.erf(z / math.sqrt(2.0)))
+    return 0.5 * z * (1 + torch.tanh(math.sqrt(2 / math.pi) * (z + 0.044715 * z * z * z)))
+
+
+def _ffn(c, x, up, down, i):
+    """Rows through expert i; a layer's rows are of its type where it holds them."""
+    if c["eight"]:
+        mid = _round_trip(_activation(x @ _weight(up, i).T, c["act"]))
+        return (mid @ _weight(down, i).T).bfloat16().float()
+    mid = _activation(x @ up[i].float().T, c["act"]).bfloat16().float()
+    return (mid @ down[i].float().T).bfloat16().float()
+
+
+def _route(c, x, W_r):
+    logits = (x.double() @ W_r.double().T).float()
+    top = torch.sort(logits, dim=1, descending=True, stable=True)
+    e = top.indices[:, :c["k"]]
+    w = torch.exp((top.values[:, :c["k"]] - top.values[:, :1]).double())
+    return e, (w / w.sum(1, keepdim=True)).float()
+
+
+def _branches(c, s, x, e, todo, rows):
+    """rows[t, p] = the output of token t's branch p where todo says so."""
+    xq = _round_trip(x) if c["eight"] else x
+    for i in range(c["E"]):
+        t, p = torch.nonzero((e == i) & todo, as_tuple=True)
+        rows[t, p] = _ffn(c, xq[t], s["up"], s["down"], i)
+    shared = torch.zeros_like(x)
+    for i in range(c["n_shared"]):
+        shared = shared + _ffn(c, xq, s["up_s"], s["down_s"], i)
+    return shared
+
+
+def _run_plain(s):
+    c = s["case"]
+    if c["kind"] == "write":
+        keep = s["slot"] >= 0
+        to = s["slot"][keep].long()
+        q, e = _quant(s["x"][keep].float())
+        s["q"][to] = q.flatten(-2).view(torch.uint8)
+        s["s"][to, :e.shape[1]] = (e + 127).to(torch.uint8)
+        s["norm"][to] = _value(q, e, c["width"]).double().square().sum(1).sqrt().float()
+        return {**_stored(s["q"], s["s"], c["width"]), "norm": s["norm"]}
+    if c["kind"] == "read":
+        at = s["slot"].long()
+        s["out"].copy_(_held(s["q"][at], s["s"][at], c["width"]))
+        return s["out"]
+    if c["kind"] == "linear":
+        y = _round_trip(s["x"].float()) @ _weight(s["w"]).T
+        s["out"].copy_(y if s["bias"] is None else y + s["bias"])
+        return s["out"]
+    T, k, d = c["B"] * c["N"], c["k"], c["d"]
+    rows = torch.zeros(T, k, d, device=DEV)
+    held_e = torch.full((T, k), -1, device=DEV)
+    held_q = torch.zeros(T, k, _pad(d, BLOCK) // BLOCK, BLOCK, dtype=torch.uint8, device=DEV)
+    held_s = torch.zeros(T, k, held_q.shape[2], dtype=torch.int32, device=DEV)
+    att_q, att_s = torch.zeros_like(held_q[:, 0]), torch.zeros_like(held_s[:, 0])
+    tok = torch.arange(T, device=DEV)[:, None].expand(T, k)
+    for t, x3 in enumerate(s["x"]):
+        x = x3.view(T, d).float()
+        e, w = _route(c, x, s["W_r"])
+        same = e[:, :, None] == held_e[:, None, :]
+        todo = ~same.any(2)
+        # a matched branch keeps its slot; the others take the free ones in order
+        free = ~same.any(1)
+        nth = (todo.cumsum(1) - 1)[:, :, None] == (free.cumsum(1) - 1)[:, None, :]
+        slot = torch.where(todo[:, :, None], nth & free[:, None, :], same).int().argmax(2)
+        cached = _value(held_q.view(torch.float8_e4m3fn), held_s, d)
+        rows = cached[tok, slot]
+        shared = _branches(c, s, x, e, todo, rows)
+        s["y"][t].copy_((shared + (w[:, :, None] * rows).sum(1)).view(x3.shape))
+        if c["kind"] == "experts":
+            return s["y"][t]
+        q, ex = _quant(rows)
+        i, p = torch.nonzero(todo, as_tuple=True)
+        held_e[i, slot[i, p]] = e[i, p]
+        held_q[i, slot[i, p]] = q[i, p].view(torch.uint8)
+        held_s[i, slot[i, p]] = ex[i, p]
+        sync = todo.any(1)
+        q, ex = _quant(s["attn"][t].view(T, d)[sync].float())
+        att_q[sync], att_s[sync] = q.view(torch.uint8), ex
+    keep = lambda q, ex: _stored(q.flatten(-2).view(-1, _pad(d, BLOCK)),  # noqa: E731
+                                 (ex + 127).to(torch.uint8).view(-1, ex.shape[-1]), d)
+    return {"y": s["y"], "cache": keep(held_q, held_s), "attention": keep(att_q, att_s)}
+
+
+def run(state):
+    return _run_own(state) if own else _run_plain(state)
+
+
+# ---------------------------------------------------------------------------
+# the definition in 64 bits
+# ---------------------------------------------------------------------------
+def _nearest(v):
+    """Nearest e4m3 numbers to v, at most 448 in magnitude: 3 bits after the leading one."""
+    _, x = torch.frexp(v)
+    step = torch.exp2((x.double() - 1).clamp(min=-6) - 3)
+    return torch.round(v / step) * step
+
+
+def _exact_rows(v):
+    """(elements, 2^e, values) of rows in 64 bits."""
+    n = -(-v.shape[-1] // BLOCK)
+    el, sc, val = torch.zeros_like(v), [], torch.zeros_like(v)
+    for b in range(n):
+        part = v[..., b * BLOCK:(b + 1) * BLOCK]
+        top = part.abs().amax(-1, keepdim=True)
+        e = torch.ceil(torch.log2(top / 448)).clamp(min=-127)
+        # the logarithm may be off by one at a power of two
+        e = torch.where(top > 448 * torch.exp2(e), e + 1, e)
+        e = torch.where((e > -127) & (top <= 448 * torch.exp2(e - 1)), e - 1, e)
+        two = torch.exp2(torch.where(top > 0, e, torch.full_like(e, -127)))
+        q = _nearest(part / two)
+        el[..., b * BLOCK:(b + 1) * BLOCK], val[..., b * BLOCK:(b + 1) * BLOCK] = q, q * two
+        sc.append(two)
+    return el, torch.cat(sc, -1), val
+
+
+def _exact_weight(w, i):
+    if not isinstance(w, dict):
+        return w[i].double()
+    el = w["q"][i].to(torch.float64)
+    out = torch.empty(w["N"], w["K"], dtype=torch.float64, device=DEV)
+    for b in range(-(-w["K"] // BLOCK)):
+        two = torch.exp2(w["s"][i, :, b].double() - 127)
+        two = two[torch.arange(w["N"], device=DEV) // BLOCK]
+        cols = slice(b * BLOCK, min(w["K"], (b + 1) * BLOCK))
+        out[:, cols] = el[:, cols] * two[:, None]
+    return out
+
+
+def _exact_ffn(c, x, up, down, i):
+    z = x @ _exact_weight(up, i).T
+    if c["act"] == "swiglu":
+        m = torch.sigmoid(z[:, ::2]) * z[:, ::2] * z[:, 1::2]
+    elif c["act"] == "gelu_erf":
+        m = z * 0.5 * torch.special.erfc(-z / math.sqrt(2.0))
+    else:
+        m = z * torch.sigmoid(2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3))
+    m = _exact_rows(m)[2] if c["eight"] else m.to(torch.bfloat16).double()
+    return (m @ _exact_weight(down, i).T).to(torch.bfloat16).double()
+
+
+def _exact_layer(c, s):
+    T, k, d = c["B"] * c["N"], c["k"], c["d"]
+    nb = -(-d // BLOCK)
+    f64 = {"dtype": torch.float64, "device": DEV}
+    ids = torch.full((T, k), -1, dtype=torch.int64, device=DEV)
+    el, sc = torch.zeros(T, k, d, **f64), torch.full((T, k, nb), 2.0 ** -127, **f64)
+    val = torch.zeros(T, k, d, **f64)
+    ael, asc = torch.zeros(T, d, **f64), torch.full((T, nb), 2.0 ** -127, **f64)
+    ys = []
+    for t in range(c["steps"]):
+        x = s["x"][t].reshape(T, d).double()
+        logits = (x @ s["W_r"].double().T).float()
+        p = torch.softmax(logits.double(), 1)
+        e = torch.argsort(logits, dim=1, descending=True, stable=True)[:, :k]
+        g = torch.gather(p, 1, e)
+        g = g / g.sum(1, keepdim=True)
+        xf = _exact_rows(x)[2] if c["eight"] else x
+        y = torch.zeros(T, d, **f64)
+        for i in range(c["n_shared"]):
+            y += _exact_ffn(c, xf, s["up_s"], s["down_s"], i)
+        # slots taken by matched branches, then a walk over the others
+        taken = torch.zeros(T, k, dtype=torch.bool, device=DEV)
+        where = torch.full((T, k), -1, dtype=torch.int64, device=DEV)
+        for j in range(k):
+            for q in range(k):
+                hit = e[:, j] == ids[:, q]
+                where[hit, j] = q
+                taken[:, q] |= hit
+        fresh = where < 0
+        for j in range(k):
+            for q in range(k):
+                use = (where[:, j] < 0) & ~taken[:, q]
+                where[use, j] = q
+                taken[:, q] |= use
+        h = torch.zeros(T, k, d, **f64)
+        for i in range(c["E"]):
+            for j in range(k):
+                r = torch.nonzero(fresh[:, j] & (e[:, j] == i))[:, 0]
+                if r.numel():
+                    h[r, j] = _exact_ffn(c, xf[r], s["up"], s["down"], i)
+        for j in range(k):
+            old = torch.nonzero(~fresh[:, j])[:, 0]
+            h[old, j] = val[old, where[old, j]]
+            y += g[:, j:j + 1] * h[:, j]
+        ys.append(y.view(c["B"], c["N"], d))
+        if c["kind"] == "experts":
+            return ys[0]
+        for j in range(k):
+            r = torch.nonzero(fresh[:, j])[:, 0]
+            q = where[r, j]
+            ids[r, q] = e[r, j]
+            el[r, q], sc[r, q], val[r, q] = _exact_rows(h[r, j])
+        r = torch.nonzero(fresh.any(1))[:, 0]
+        ael[r], asc[r], _ = _exact_rows(s["attn"][t].reshape(T, d)[r].double())
+    return {"y": ys, "cache": {"elements": el.view(T * k, d), "scales": sc.view(T * k, nb)},
+            "attention": {"elements": ael, "scales": asc}}
+
+
+def exact(case, seed):
+    global own
+    c, was = case, own
+    own = False
+    try:
+        s = prepare(case, seed)
+    finally:
+        own = was
+    if c["kind"] == "write":
+        el, sc = torch.zeros(c["slots"], c["width"], dtype=torch.float64, device=DEV), None
+        sc = torch.full((c["slots"], -(-c["width"] // BLOCK)), 2.0 ** -127, dtype=torch.float64,
+                        device=DEV)
+        norm = torch.zeros(c["slots"], dtype=torch.float64, device=DEV)
+        r = torch.nonzero(s["slot"] >= 0)[:, 0]
+        to = s["slot"][r].long()
+        el[to], sc[to], val = _exact_rows(s["x"][r].double())
+        norm[to] = torch.linalg.vector_norm(val, dim=1)
+        return {"elements": el, "scales": sc, "norm": norm}
+    if c["kind"] == "read":
+        at = s["slot"].long()
+        nb = -(-c["width"] // BLOCK)
+        two = torch.exp2(s["s"][at].double() - 127)
+        col = torch.arange(c["width"], device=DEV) // BLOCK
+        return s["q"].view(torch.float8_e4m3fn)[at, :c["width"]].double() * two[:, :nb][:, col]
+    if c["kind"] == "linear":
+        y = _exact_rows(s["x"].double())[2] @ _exact_weight(s["w"], 0).T
+        return y if s["bias"] is None else y + s["bias"].double()
+    return _exact_layer(c, s)
