@@ -128,7 +128,7 @@ def work(case):
     if c["kind"] in ("write", "read"):
         size = 2 if c["dtype"] == "bf16" else 4
         blocks = -(-c["width"] // BLOCK)
-        kept = int(0.9 * c["rows"]) if c["kind"] == "write" else c["rows"]
+        kept = -(-9 * c["rows"] // 10) if c["kind"] == "write" else c["rows"]
         each = c["width"] * (size + 1) + blocks + 4
         return {"bytes": kept * (each + (4 if c["kind"] == "write" else 0)),
                 "flops": kept * c["width"] * (4 if c["kind"] == "write" else 1)}
