@@ -129,6 +129,43 @@ int moeca_layer_set_weights(moeca_layer* layer, const void* W_r, const float* b_
  * NULL or not 16-byte aligned. */
 int moeca_layer_set_shared(moeca_layer* layer, const void* W_up_s, const void* W_down_s);
 
+/* Hold the layer's expert weights and hidden rows, its cache, or both in 8
+ * bits (the stored form of the section on 8-bit rows and matrices below).
+ *   MOECA_QUANT_EXPERTS  the step quantises its FFN input, multiplies 8-bit
+ *     operands, and quantises each expert's hidden rows act(W_up x) from their
+ *     fp32 values; the down projection's rows are of the policy dtype as
+ *     before.  Shared experts are held the same way, the router is not.  The
+ *     weights are bound with moeca_layer_set_weights_quant() (and
+ *     moeca_layer_set_shared_quant()) in the place of the plain calls.
+ *   MOECA_QUANT_CACHE    cached branch rows are 8-bit, their norms those of the
+ *     stored values; a step's output takes a recomputed branch's row as the
+ *     down projection left it and a reused branch's as stored.  An attention
+ *     path is bound with moeca_bind_attention_quant().  Not for FULL mode,
+ *     which has no cache.
+ * flags replaces what was set before (0: neither).  A change unbinds the
+ * workspace, whose size changes (call moeca_workspace_bytes() and
+ * moeca_bind_workspace() afterwards), the weights if it is one of EXPERTS, and
+ * the attention path if it is one of CACHE.  Host only.  MOECA_E_INVAL: NULL
+ * layer, unknown flags, CACHE in FULL mode; MOECA_E_STATE: the layer is a block
+ * of a stack. */
+enum { MOECA_QUANT_EXPERTS = 1, MOECA_QUANT_CACHE = 2 };
+int moeca_layer_set_quant(moeca_layer* layer, int flags);
+
+/* Bind the weights of a layer with MOECA_QUANT_EXPERTS (device, not copied):
+ * W_r and b_r as in moeca_layer_set_weights(), and, as moeca_quant_matrix()
+ * writes them,
+ *   up,   up_scale    E matrices of U rows and d inputs
+ *   down, down_scale  E matrices of d rows and d_ff inputs
+ * MOECA_E_INVAL if a required pointer is NULL or not 16-byte aligned (the bias
+ * 4-byte), or the layer's experts are not quantised. */
+int moeca_layer_set_weights_quant(moeca_layer* layer, const void* W_r, const float* b_r,
+                                  const void* up, const void* up_scale, const void* down,
+                                  const void* down_scale);
+
+/* The shared experts' weights of such a layer: S matrices in the place of E. */
+int moeca_layer_set_shared_quant(moeca_layer* layer, const void* up, const void* up_scale,
+                                 const void* down, const void* down_scale);
+
 /* Bytes of device workspace the layer needs: the branch cache (ids, gate
  * weights, norms and rows of B*N*k branches), the EMA statistic [B][E][N],
  * and per-step scratch (routing, scores, masks, expert lists, the FFN
@@ -150,6 +187,14 @@ int moeca_bind_workspace(moeca_layer* layer, void* dev, size_t bytes);
  * each step's features into the same buffer.  Both NULL unbinds; one NULL,
  * or a pointer that is not 16-byte aligned, is MOECA_E_INVAL. */
 int moeca_bind_attention(moeca_layer* layer, const void* attn_in, void* attn_cache);
+
+/* The attention path of a layer with MOECA_QUANT_CACHE: as
+ * moeca_bind_attention(), but row i of the attention cache is quantised as it
+ * is written, into q [B*N][moeca_quant_pitch(d)] and scale
+ * [B*N][moeca_quant_scale_pitch(d)] (device); moeca_dequant_rows() reads rows
+ * back.  All NULL unbinds; some NULL, or a pointer that is not 16-byte aligned,
+ * is MOECA_E_INVAL, and so is a layer whose cache is not quantised. */
+int moeca_bind_attention_quant(moeca_layer* layer, const void* attn_in, void* q, void* scale);
 
 /* One layer step at sampling step t (0-based).
  *   x_t [B][N][d]  device, policy dtype: the MoE layer input u of Sec. 2.3
@@ -236,7 +281,8 @@ enum {
   MOECA_BUF_E_C = 0,    /* int32 [B*N*k]    cached expert id, -1 = empty      */
   MOECA_BUF_W_C = 1,    /* fp32  [B*N*k]    cached gate weight w^{t0}         */
   MOECA_BUF_N_C = 2,    /* fp32  [B*N*k]    norm of the cached row ||h^{t0}|| */
-  MOECA_BUF_H_C = 3,    /* act   [B*N*k][d] cached branch outputs h^{t0}      */
+  MOECA_BUF_H_C = 3,    /* act   [B*N*k][d] cached branch outputs h^{t0}; with
+                           MOECA_QUANT_CACHE uint8 [B*N*k][pitch], e4m3       */
   MOECA_BUF_STAT = 4,   /* fp32  [B][E][N]  EMA statistic C_{e,i}             */
   MOECA_BUF_LOGITS = 5, /* fp32  [B*N][E]   router logits of the last step    */
   MOECA_BUF_E_T = 6,    /* int32 [B*N*k]    current experts e_{i,p}           */
@@ -254,7 +300,9 @@ enum {
   MOECA_BUF_LIST = 16,  /* int32 [B*N*k]    recomputed flat branch ids
                            f = (b*N + i)*k + p, grouped by expert, ascending  */
   MOECA_BUF_POS = 17,   /* int32 [B*N*k]    index of f in LIST, -1 if reused  */
-  MOECA_BUF_COUNT = 18
+  MOECA_BUF_S_C = 18,   /* uint8 [B*N*k][scale pitch] scales of the cached rows
+                           (MOECA_QUANT_CACHE; else empty)                    */
+  MOECA_BUF_COUNT = 19
 };
 
 /* Byte offset and size of an internal buffer inside the bound workspace, for
@@ -296,6 +344,62 @@ int moeca_set_timing(moeca_layer* layer, int enable);
  * stage skipped on a step contributes 0.  *steps receives the number of
  * steps.  Synchronises the recorded events and clears the record. */
 int moeca_get_timing(moeca_layer* layer, double* ms, int n, int* steps);
+
+/* ---- 8-bit rows and matrices --------------------------------------------
+ * The stored form: e4m3 elements (OCP; the largest finite number is 448, NaN is
+ * 0x7f, there are no infinities) with a power-of-two scale 2^e for each block of
+ * 128, held as the byte e + 127.  A block is 128 consecutive elements of a row,
+ * or 128 x 128 elements of a weight matrix; the last ones may be smaller.  e is
+ * the smallest integer, not below -127, for which the block's largest finite
+ * magnitude is at most 448 2^e; an element is the e4m3 number nearest to v 2^-e
+ * (ties to even), and stands for that number times 2^e.  NaN and infinities
+ * become NaN.  A value within 2^-4 of the largest fp32 number may round up to
+ * 2^128 and be read back as infinity.
+ *   elements  [rows][moeca_quant_pitch(K)]        K rounded up to 128, the rest zeros
+ *   scales    [rows][moeca_quant_scale_pitch(K)]  a byte per block, rounded up to 16
+ *             bytes, the rest unspecified (a matrix: ceil(N / 128) such rows)
+ * Elements and scales must be 16-byte aligned.  Rows of the activation type
+ * (dtype MOECA_DTYPE_*) have a stride of ld >= K elements and the alignment of
+ * their type; 16-byte aligned rows are faster.  K and N are in [1, 1048576].
+ * Calls enqueue on the stream; they neither allocate nor wait.  Buffers that a
+ * call writes must not overlap the ones it reads. */
+size_t moeca_quant_pitch(int64_t K);       /* bytes; 0 if K < 1 */
+size_t moeca_quant_scale_pitch(int64_t K); /* bytes; 0 if K < 1 */
+
+/* Quantise rows as they are written into slots: row r of src goes to row
+ * slot[r] of q and scale (slot NULL: row r), and norm[slot[r]] (optional)
+ * becomes the L2 norm of the stored values, an fp64 sum rounded once.  A row
+ * whose slot is outside [0, slots) is left out, and slots that no row goes to
+ * keep what they hold.  Two rows with the same slot leave an unspecified mix of
+ * both there.  rows = 0 does nothing.  MOECA_E_INVAL: sizes out of range, more
+ * rows than slots without indexes, NULL or misaligned pointers. */
+int moeca_quant_rows(const void* src, int dtype, int64_t rows, int64_t K, int64_t ld,
+                     const int32_t* slot, int64_t slots, void* q, void* scale, float* norm,
+                     void* stream);
+
+/* Read rows back: row r of dst becomes the values of row slot[r] (slot NULL:
+ * row r), rounded to dtype; a slot outside [0, slots) gives zeros.  Elements of
+ * dst past K keep what they hold. */
+int moeca_dequant_rows(const void* q, const void* scale, int64_t slots, int64_t K,
+                       const int32_t* slot, int64_t rows, void* dst, int dtype, int64_t ld,
+                       void* stream);
+
+/* Quantise `count` dense weight matrices W [count][N][K] (out x in): q
+ * [count][N][pitch], scale [count][ceil(N / 128)][scale pitch]. */
+int moeca_quant_matrix(const void* W, int dtype, int64_t count, int64_t N, int64_t K, void* q,
+                       void* scale, void* stream);
+
+/* out = x W^T (+ bias) for rows x [M][K] of the activation type, quantised by
+ * the call, and a quantised matrix W of N rows: products of 8-bit operands with
+ * both scales, fp32 sums, the bias (fp32 [N], or NULL) added in fp32, one
+ * rounding to dtype.  workspace: moeca_quant_linear_bytes(M, K) bytes, 256-byte
+ * aligned, for the quantised rows; calls that overlap in time need one each.
+ * M = 0 does nothing.  A row's sums do not depend on the other rows of the
+ * call, except that M may choose another order of the sums over K. */
+size_t moeca_quant_linear_bytes(int64_t M, int64_t K);
+int moeca_quant_linear(const void* x, int dtype, int64_t M, int64_t K, int64_t ldx, const void* q,
+                       const void* scale, int64_t N, const float* bias, void* out, int64_t ldo,
+                       void* workspace, size_t bytes, void* stream);
 
 /* ---- DiT-MoE block stack ----------------------------------------------
  * L DiT-MoE blocks (Sec. 2.1, composition eq. and residual form; the MoE FFN

@@ -18,11 +18,12 @@ MOECA_E_HIP = -3
 MOECA_MODE_FULL, MOECA_MODE_THRESHOLD, MOECA_MODE_RATIO = 0, 1, 2
 MOECA_DTYPE_BF16, MOECA_DTYPE_FP32 = 0, 1
 MOECA_ACT_GELU_TANH, MOECA_ACT_GELU_ERF, MOECA_ACT_SWIGLU = 0, 1, 2
+MOECA_QUANT_EXPERTS, MOECA_QUANT_CACHE = 1, 2
 
 BUF = {
     "e_c": 0, "w_c": 1, "n_c": 2, "h_c": 3, "stat": 4, "logits": 5, "e_t": 6, "w_t": 7,
     "hbar": 8, "tau": 9, "margin": 10, "q": 11, "mask": 12, "sigma": 13, "sync": 14,
-    "off": 15, "list": 16, "pos": 17,
+    "off": 15, "list": 16, "pos": 17, "s_c": 18,
 }
 STAGES = ["router", "stat", "select", "lists", "ffn_up", "ffn_down", "combine"]
 SBUF = {
@@ -59,6 +60,7 @@ class moeca_block_weights(ctypes.Structure):
 
 
 _vp = ctypes.c_void_p
+_i64 = ctypes.c_int64
 _SIGS = {
     "moeca_policy_default": (None, [ctypes.POINTER(moeca_policy)]),
     "moeca_layer_create": (ctypes.c_void_p, [ctypes.c_int, ctypes.c_int, ctypes.c_int,
@@ -86,6 +88,20 @@ _SIGS = {
     "moeca_set_timing": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int]),
     "moeca_get_timing": (ctypes.c_int, [ctypes.c_void_p, ctypes.POINTER(ctypes.c_double),
                                         ctypes.c_int, ctypes.POINTER(ctypes.c_int)]),
+    "moeca_layer_set_quant": (ctypes.c_int, [_vp, ctypes.c_int]),
+    "moeca_layer_set_weights_quant": (ctypes.c_int, [_vp] * 7),
+    "moeca_layer_set_shared_quant": (ctypes.c_int, [_vp] * 5),
+    "moeca_bind_attention_quant": (ctypes.c_int, [_vp] * 4),
+    "moeca_quant_pitch": (ctypes.c_size_t, [_i64]),
+    "moeca_quant_scale_pitch": (ctypes.c_size_t, [_i64]),
+    "moeca_quant_rows": (ctypes.c_int, [_vp, ctypes.c_int, _i64, _i64, _i64, _vp, _i64, _vp, _vp,
+                                        _vp, _vp]),
+    "moeca_dequant_rows": (ctypes.c_int, [_vp, _vp, _i64, _i64, _vp, _i64, _vp, ctypes.c_int,
+                                          _i64, _vp]),
+    "moeca_quant_matrix": (ctypes.c_int, [_vp, ctypes.c_int, _i64, _i64, _i64, _vp, _vp, _vp]),
+    "moeca_quant_linear_bytes": (ctypes.c_size_t, [_i64, _i64]),
+    "moeca_quant_linear": (ctypes.c_int, [_vp, ctypes.c_int, _i64, _i64, _i64, _vp, _vp, _i64,
+                                          _vp, _vp, _i64, _vp, ctypes.c_size_t, _vp]),
     "moeca_stack_create": (_vp, [ctypes.c_int] * 6 + [ctypes.POINTER(moeca_policy)]),
     "moeca_stack_destroy": (None, [_vp]),
     "moeca_stack_set_block": (ctypes.c_int, [_vp, ctypes.c_int,
@@ -212,6 +228,56 @@ def moeca_get_timing(h, n: int = 7) -> tuple[list[float], int]:
     steps = ctypes.c_int()
     _check(load().moeca_get_timing(h, arr, n, ctypes.byref(steps)))
     return list(arr), steps.value
+
+
+# ---- 8-bit rows and matrices -----------------------------------------------
+def moeca_layer_set_quant(h, flags: int) -> int:
+    return _check(load().moeca_layer_set_quant(h, flags))
+
+
+def moeca_layer_set_weights_quant(h, W_r, b_r, up, up_scale, down, down_scale) -> int:
+    return _check(load().moeca_layer_set_weights_quant(h, W_r, b_r, up, up_scale, down,
+                                                       down_scale))
+
+
+def moeca_layer_set_shared_quant(h, up, up_scale, down, down_scale) -> int:
+    return _check(load().moeca_layer_set_shared_quant(h, up, up_scale, down, down_scale))
+
+
+def moeca_bind_attention_quant(h, attn_in, q, scale) -> int:
+    return _check(load().moeca_bind_attention_quant(h, attn_in, q, scale))
+
+
+def moeca_quant_pitch(K: int) -> int:
+    return load().moeca_quant_pitch(K)
+
+
+def moeca_quant_scale_pitch(K: int) -> int:
+    return load().moeca_quant_scale_pitch(K)
+
+
+def moeca_quant_rows(src, dtype, rows, K, ld, slot, slots, q, scale, norm, stream) -> int:
+    return _check(load().moeca_quant_rows(src, dtype, rows, K, ld, slot, slots, q, scale, norm,
+                                          stream))
+
+
+def moeca_dequant_rows(q, scale, slots, K, slot, rows, dst, dtype, ld, stream) -> int:
+    return _check(load().moeca_dequant_rows(q, scale, slots, K, slot, rows, dst, dtype, ld,
+                                            stream))
+
+
+def moeca_quant_matrix(W, dtype, count, N, K, q, scale, stream) -> int:
+    return _check(load().moeca_quant_matrix(W, dtype, count, N, K, q, scale, stream))
+
+
+def moeca_quant_linear_bytes(M: int, K: int) -> int:
+    return load().moeca_quant_linear_bytes(M, K)
+
+
+def moeca_quant_linear(x, dtype, M, K, ldx, q, scale, N, bias, out, ldo, workspace, nbytes,
+                       stream) -> int:
+    return _check(load().moeca_quant_linear(x, dtype, M, K, ldx, q, scale, N, bias, out, ldo,
+                                            workspace, nbytes, stream))
 
 
 # ---- block stack -----------------------------------------------------------

@@ -35,6 +35,9 @@ SOURCES = {
     "ffn.hip": [],
     "block.hip": ["-ffp-contract=off"],
     "noalloc.hip": [],
+    "qrows.hip": ["-ffp-contract=off"],
+    "qgemm.hip": [],
+    "quant.cpp": [],
     "moeca.cpp": ["-ffp-contract=off"],
     "stack.cpp": [],
 }

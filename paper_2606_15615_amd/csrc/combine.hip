@@ -408,7 +408,7 @@ __global__ __launch_bounds__(kCombWaves * kWave) void combine_wide_kernel(
 }  // namespace
 
 bool combine_sums(const Shape& s) {
-  return s.k <= 2 && (s.d / 8 + kWave - 1) / kWave <= 4 && s.S == 0 &&
+  return s.k <= 2 && (s.d / 8 + kWave - 1) / kWave <= 4 && s.S == 0 && !s.cache8 &&
          s.tokens() < (int64_t(1) << 31);
 }
 

@@ -126,6 +126,7 @@ __device__ __forceinline__ bool token_slots(const int8_t* sq, const uint8_t* sm,
 struct ListArgs {
   int S, T;  // shared experts, tokens of the batch
   int tm_up, tm, nt_up, nt_down, tall_up, tall_down, cus;
+  int in_list;  // the down projection leaves its rows in list order (row_dst = identity)
   int32_t *off, *tiles, *list, *pos, *row_dst;
 };
 
@@ -642,7 +643,7 @@ __global__ __launch_bounds__(kSelThreads) void decide_kernel(
       for (int w2 = 0; w2 < wv; ++w2) idx += s_wcnt[r][w2][e];
       la.list[idx] = j;
       la.pos[j] = idx;
-      la.row_dst[idx] = j / k * k + s_q[j];
+      la.row_dst[idx] = la.in_list ? idx : j / k * k + s_q[j];
     }
   }
   if (tid < E) cnt_bs[b * E + tid] = s_cnt[tid];
@@ -747,7 +748,7 @@ __global__ __launch_bounds__(kSelThreads) void lists_kernel(
   const int idx = s_base[ev] + before + rk;
   la.list[idx] = static_cast<int32_t>(f);
   la.pos[f] = idx;
-  la.row_dst[idx] = static_cast<int32_t>((f / k) * k + sg);
+  la.row_dst[idx] = la.in_list ? idx : static_cast<int32_t>((f / k) * k + sg);
 }
 
 // ---------------------------------------------------------------------------
@@ -1161,8 +1162,8 @@ static ListArgs list_args(const Shape& s, const FfnPlan& plan, const Buffers& b)
   return ListArgs{s.S, static_cast<int>(s.tokens()), plan.tm_up, plan.tm,
                   (s.up_rows() + plan.tn_up - 1) / plan.tn_up,
                   (s.d + plan.tn_down - 1) / plan.tn_down * plan.split_down,
-                  plan.tall_up ? 1 : 0, plan.tall_down ? 1 : 0, device_cus(), b.off, b.tiles,
-                  b.list, b.pos, b.row_dst};
+                  plan.tall_up ? 1 : 0, plan.tall_down ? 1 : 0, device_cus(), s.cache8 ? 1 : 0,
+                  b.off, b.tiles, b.list, b.pos, b.row_dst};
 }
 
 // Every wave ranks its branches by a ballot per expert, which the launch of its

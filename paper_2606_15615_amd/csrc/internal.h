@@ -14,8 +14,8 @@ namespace moeca {
 
 // Launch timing.  When `start` is set, the next kernel launched through
 // launch_kernel records the two events as part of its own dispatch (its
-// start and completion timestamps, with no marker packets in between), and
-// the slot is cleared.  Per host thread.
+// start and completion timestamps, with no marker packets in between; either
+// may be null), and the slot is cleared.  Per host thread.
 struct LaunchEvents {
   hipEvent_t start = nullptr;
   hipEvent_t stop = nullptr;
@@ -26,7 +26,7 @@ template <typename... P, typename... A>
 inline void launch_kernel(void (*kernel)(P...), dim3 grid, dim3 block, uint32_t shmem,
                           hipStream_t st, A... args) {
   LaunchEvents& ev = launch_events();
-  if (ev.start != nullptr) {
+  if (ev.start != nullptr || ev.stop != nullptr) {
     hipExtLaunchKernelGGL(kernel, grid, block, shmem, st, ev.start, ev.stop, 0u,
                           static_cast<P>(args)...);
     ev = LaunchEvents{};
@@ -58,6 +58,8 @@ struct Shape {
   int S = 0;            // shared experts
   bool swiglu = false;  // gated experts: 2 d_ff up-projection rows
   bool erf = false;     // erf GELU
+  bool experts8 = false;  // expert weights and hidden rows in 8 bits (q8.h)
+  bool cache8 = false;    // cache rows in 8 bits
   int64_t tokens() const { return int64_t(B) * N; }
   int64_t branches() const { return int64_t(B) * N * k; }
   size_t act_bytes() const { return bf16 ? 2 : 4; }
@@ -100,6 +102,9 @@ struct Buffers {
   int32_t* wide;    // [B][kWideWords] per-sample scratch of the multi-block decision path
   void* mid;        // [B*N*k + S*T][d_ff] FFN activation of listed and shared rows
   void* h_sh;       // [S][T][d] shared experts' outputs
+  uint8_t* s_c;     // cache8: [B*N*k][spitch] scales of the cache rows
+  void* fresh;      // cache8: [B*N*k][d] rows of the down projection, list order
+  void* x8;         // experts8: the step's FFN input, quantised (q8_view)
   float* part;      // [pieces][B*N*k][d] fp32 partial sums of the down projection's K
                     // pieces: kThinSplit (layers that may take the weight-streaming
                     // plan) or f32_split (fp32 layers); null: K is not split
@@ -185,6 +190,40 @@ hipError_t launch_combine(const Shape& s, int write_cache, int pieces, void* out
                           hipStream_t st);
 bool combine_sums(const Shape& s);
 hipError_t launch_reset(const Shape& s, const Buffers& b, hipStream_t st);
+
+// ---- 8-bit rows and products (qrows.hip, qgemm.hip) ----------------------
+// Quantised rows: elements [rows][pitch] and, 256-byte aligned behind them,
+// scales [rows][spitch].
+struct Q8 {
+  uint8_t *q, *s;
+};
+size_t q8_bytes(int64_t rows, int64_t K);
+Q8 q8_view(void* base, int64_t rows, int64_t K);
+// A layer's 8-bit expert weights (elements and scales, shared experts' too).
+struct QuantWeights {
+  const void *up = nullptr, *up_s = nullptr, *down = nullptr, *down_s = nullptr;
+  const void *up_sh = nullptr, *up_sh_s = nullptr, *down_sh = nullptr, *down_sh_s = nullptr;
+};
+hipError_t launch_quant_rows(const void* src, bool bf16, int64_t rows, int K, int64_t ld,
+                             const int32_t* slot, int64_t slots, uint8_t* q, uint8_t* s,
+                             float* norm, hipStream_t st);
+hipError_t launch_dequant_rows(const uint8_t* q, const uint8_t* s, int64_t slots, int K,
+                               const int32_t* slot, int64_t rows, void* dst, bool bf16,
+                               int64_t ld, hipStream_t st);
+hipError_t launch_quant_matrix(const void* W, bool bf16, int count, int N, int K, uint8_t* q,
+                               uint8_t* s, hipStream_t st);
+// The combine of a cache8 layer: recomputed rows from b.fresh into the cache.
+hipError_t launch_combine_q8(const Shape& s, void* out, const void* attn_in, uint8_t* attn_q,
+                             uint8_t* attn_s, const Buffers& b, hipStream_t st);
+FfnPlan q8_plan(const Shape& s, StepKind kind, int64_t rows);
+hipError_t launch_q8_up(const Shape& s, int act, const FfnPlan& plan, const QuantWeights& w,
+                        const Buffers& b, hipStream_t st);
+hipError_t launch_q8_down(const Shape& s, const FfnPlan& plan, const QuantWeights& w,
+                          const Buffers& b, hipStream_t st);
+// out = values(x) W^T (+ bias), x of M rows, W of N
+hipError_t launch_q8_linear(const Q8& x, int64_t M, int K, const void* W, const void* Ws, int N,
+                            const float* bias, void* out, bool bf16, int64_t ldo,
+                            hipStream_t st);
 
 // ---- the entry point that allocates nothing (noalloc.hip) --------------
 // Bytes of the library-owned device array every call of

@@ -46,8 +46,8 @@ size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 // Workspace regions, in order.  Public ids come first (MOECA_BUF_*).
 enum Region {
   R_E_C, R_W_C, R_N_C, R_H_C, R_STAT, R_LOGITS, R_E_T, R_W_T, R_HBAR, R_TAU, R_MARGIN, R_Q,
-  R_MASK, R_SIGMA, R_SYNC, R_OFF, R_LIST, R_POS,
-  R_CNT_BS, R_STATS_BS, R_RFLAGS, R_TILES, R_ROW_DST, R_ENT, R_CNT_CH, R_WIDE, R_MID, R_H_SH,
+  R_MASK, R_SIGMA, R_SYNC, R_OFF, R_LIST, R_POS, R_S_C,
+  R_FRESH, R_X8, R_CNT_BS, R_STATS_BS, R_RFLAGS, R_TILES, R_ROW_DST, R_ENT, R_CNT_CH, R_WIDE, R_MID, R_H_SH,
   R_PART, R_COUNT
 };
 
@@ -56,6 +56,12 @@ struct Layout {
   size_t bytes[R_COUNT];
   size_t total;
 };
+
+// Bytes of the FFN intermediate.
+size_t mid_bytes(const Shape& s) {
+  return s.experts8 ? moeca::q8_bytes(s.mid_rows(), s.d_ff)
+                    : size_t(s.mid_rows()) * s.d_ff * s.act_bytes();
+}
 
 // external_mid: the FFN intermediate lives outside this workspace (the
 // blocks of a stack run one after another and share one).  partials: room
@@ -68,7 +74,10 @@ Layout make_layout(const Shape& s, bool external_mid = false, bool partials = tr
   b[R_E_C] = nbr * 4;
   b[R_W_C] = nbr * 4;
   b[R_N_C] = nbr * 4;
-  b[R_H_C] = nbr * s.d * act;
+  b[R_H_C] = s.cache8 ? nbr * moeca_quant_pitch(s.d) : nbr * s.d * act;
+  b[R_S_C] = s.cache8 ? nbr * moeca_quant_scale_pitch(s.d) : 0;
+  b[R_FRESH] = s.cache8 ? nbr * s.d * act : 0;
+  b[R_X8] = s.experts8 ? moeca::q8_bytes(s.tokens(), s.d) : 0;
   b[R_STAT] = size_t(s.B) * s.E * s.N * 4;
   b[R_LOGITS] = ntok * s.E * 4;
   b[R_E_T] = nbr * 4;
@@ -91,9 +100,9 @@ Layout make_layout(const Shape& s, bool external_mid = false, bool partials = tr
   b[R_ENT] = size_t(s.B) * s.E * ((size_t(s.N) + 15) / 16) * 2 * 8;
   b[R_CNT_CH] = size_t(s.B) * ((size_t(s.N) * s.k + 1023) / 1024) * s.E * 4;
   b[R_WIDE] = size_t(s.B) * moeca::kWideWords * 4;
-  b[R_MID] = external_mid ? 0 : size_t(s.mid_rows()) * s.d_ff * act;
+  b[R_MID] = external_mid ? 0 : mid_bytes(s);
   b[R_H_SH] = size_t(s.S) * ntok * s.d * act;
-  const int pieces = !partials                   ? 1
+  const int pieces = !partials || s.experts8    ? 1
                      : moeca::thin_capable(s) ? moeca::kThinSplit
                                               : moeca::f32_split(s);
   b[R_PART] = pieces > 1 ? size_t(pieces) * size_t(s.mid_rows()) * s.d * 4 : 0;
@@ -143,6 +152,9 @@ Buffers map_buffers(char* w, const Layout& lay, void* mid) {
   b.row_dst = reinterpret_cast<int32_t*>(w + o[R_ROW_DST]);
   b.mid = mid != nullptr ? mid : w + o[R_MID];
   b.h_sh = w + o[R_H_SH];
+  b.s_c = reinterpret_cast<uint8_t*>(w + o[R_S_C]);
+  b.fresh = w + o[R_FRESH];
+  b.x8 = w + o[R_X8];
   b.part = lay.bytes[R_PART] != 0 ? reinterpret_cast<float*>(w + o[R_PART]) : nullptr;
   return b;
 }
@@ -159,10 +171,12 @@ struct moeca_layer {
   const void* W_down = nullptr;
   const void* W_up_sh = nullptr;
   const void* W_down_sh = nullptr;
+  moeca::QuantWeights qw;  // experts8: in the place of W_up, W_down and the shared ones
   char* ws = nullptr;
   Buffers buf{};
   const void* attn_in = nullptr;
   void* attn_cache = nullptr;
+  uint8_t *attn_q = nullptr, *attn_s = nullptr;  // cache8: in the place of attn_cache
   bool valid = false;
   bool mid_outside = false;      // the FFN intermediate is not in ws
   void* external_mid = nullptr;  // its address when mid_outside
@@ -172,6 +186,37 @@ struct moeca_layer {
   std::vector<hipEvent_t> events;
   int timed_steps = 0;
 };
+
+namespace {
+
+bool shared_bound(const moeca_layer* L) {
+  return L->shape.S == 0 || (L->shape.experts8 ? L->qw.up_sh : L->W_up_sh) != nullptr;
+}
+
+// The expert FFN's two projections; experts8: the input is quantised first, in a
+// launch that carries the stage's start event while the product carries its
+// stop event.
+hipError_t ffn_up(const moeca_layer* L, const Shape& s, const void* x, const moeca::FfnPlan& plan,
+                  const Buffers& b, hipStream_t st) {
+  if (!s.experts8)
+    return moeca::launch_ffn_up(s, x, L->W_up, L->W_up_sh, L->pol.act, plan, b, st);
+  const moeca::LaunchEvents ev = moeca::launch_events();
+  moeca::launch_events() = {ev.start, nullptr};
+  const moeca::Q8 q = moeca::q8_view(b.x8, s.tokens(), s.d);
+  const hipError_t e = moeca::launch_quant_rows(x, s.bf16, s.tokens(), s.d, s.d, nullptr,
+                                                s.tokens(), q.q, q.s, nullptr, st);
+  if (e != hipSuccess) return e;
+  moeca::launch_events() = {nullptr, ev.stop};
+  return moeca::launch_q8_up(s, L->pol.act, plan, L->qw, b, st);
+}
+
+hipError_t ffn_down(const moeca_layer* L, const Shape& s, const moeca::FfnPlan& plan,
+                    const Buffers& b, hipStream_t st) {
+  if (s.experts8) return moeca::launch_q8_down(s, plan, L->qw, b, st);
+  return moeca::launch_ffn_down(s, L->W_down, L->W_down_sh, plan, b, st);
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -252,6 +297,8 @@ void moeca_layer_destroy(moeca_layer* L) {
 int moeca_layer_set_weights(moeca_layer* L, const void* W_r, const float* b_r, const void* W_up,
                             const void* W_down) {
   if (L == nullptr) return fail(MOECA_E_INVAL, "layer is NULL");
+  if (L->shape.experts8)
+    return fail(MOECA_E_INVAL, "the layer's experts are quantised: moeca_layer_set_weights_quant");
   if (W_r == nullptr || W_up == nullptr || W_down == nullptr)
     return fail(MOECA_E_INVAL, "W_r, W_up and W_down are required");
   if (!aligned16(W_r) || !aligned16(W_up) || !aligned16(W_down) ||
@@ -267,12 +314,80 @@ int moeca_layer_set_weights(moeca_layer* L, const void* W_r, const float* b_r, c
 int moeca_layer_set_shared(moeca_layer* L, const void* W_up_s, const void* W_down_s) {
   if (L == nullptr) return fail(MOECA_E_INVAL, "layer is NULL");
   if (L->shape.S == 0) return fail(MOECA_E_INVAL, "the layer has no shared experts");
+  if (L->shape.experts8)
+    return fail(MOECA_E_INVAL, "the layer's experts are quantised: moeca_layer_set_shared_quant");
   if (W_up_s == nullptr || W_down_s == nullptr)
     return fail(MOECA_E_INVAL, "W_up_s and W_down_s are required");
   if (!aligned16(W_up_s) || !aligned16(W_down_s))
     return fail(MOECA_E_INVAL, "shared weights must be 16-byte aligned");
   L->W_up_sh = W_up_s;
   L->W_down_sh = W_down_s;
+  return MOECA_OK;
+}
+
+int moeca_layer_set_quant(moeca_layer* L, int flags) {
+  if (L == nullptr) return fail(MOECA_E_INVAL, "layer is NULL");
+  if ((flags & ~(MOECA_QUANT_EXPERTS | MOECA_QUANT_CACHE)) != 0)
+    return fail(MOECA_E_INVAL, "unknown quantisation flag");
+  if ((flags & MOECA_QUANT_CACHE) != 0 && L->pol.mode == MOECA_MODE_FULL)
+    return fail(MOECA_E_INVAL, "an uncached layer has no cache to quantise");
+  if (L->mid_outside)
+    return fail(MOECA_E_STATE, "the layer is a block of a stack, which has laid its workspace out");
+  const bool experts = (flags & MOECA_QUANT_EXPERTS) != 0, cache = (flags & MOECA_QUANT_CACHE) != 0;
+  if (experts == L->shape.experts8 && cache == L->shape.cache8) return MOECA_OK;
+  if (experts != L->shape.experts8) {
+    L->W_r = L->W_up = L->W_down = L->W_up_sh = L->W_down_sh = nullptr;
+    L->b_r = nullptr;
+    L->qw = moeca::QuantWeights{};
+  }
+  if (cache != L->shape.cache8) {
+    L->attn_in = nullptr;
+    L->attn_cache = nullptr;
+    L->attn_q = L->attn_s = nullptr;
+  }
+  L->shape.experts8 = experts;
+  L->shape.cache8 = cache;
+  L->layout = make_layout(L->shape);
+  L->ws = nullptr;  // the layout changed: bind again
+  L->valid = false;
+  return MOECA_OK;
+}
+
+int moeca_layer_set_weights_quant(moeca_layer* L, const void* W_r, const float* b_r,
+                                  const void* up, const void* up_scale, const void* down,
+                                  const void* down_scale) {
+  if (L == nullptr) return fail(MOECA_E_INVAL, "layer is NULL");
+  if (!L->shape.experts8)
+    return fail(MOECA_E_INVAL, "the layer's experts are not quantised (moeca_layer_set_quant)");
+  if (W_r == nullptr || up == nullptr || up_scale == nullptr || down == nullptr ||
+      down_scale == nullptr)
+    return fail(MOECA_E_INVAL, "W_r and the experts' elements and scales are required");
+  if (!aligned16(W_r) || !aligned16(up) || !aligned16(up_scale) || !aligned16(down) ||
+      !aligned16(down_scale) || (reinterpret_cast<uintptr_t>(b_r) & 3u) != 0)
+    return fail(MOECA_E_INVAL, "weights must be 16-byte aligned (bias 4-byte)");
+  L->W_r = W_r;
+  L->b_r = b_r;
+  L->qw.up = up;
+  L->qw.up_s = up_scale;
+  L->qw.down = down;
+  L->qw.down_s = down_scale;
+  return MOECA_OK;
+}
+
+int moeca_layer_set_shared_quant(moeca_layer* L, const void* up, const void* up_scale,
+                                 const void* down, const void* down_scale) {
+  if (L == nullptr) return fail(MOECA_E_INVAL, "layer is NULL");
+  if (L->shape.S == 0) return fail(MOECA_E_INVAL, "the layer has no shared experts");
+  if (!L->shape.experts8)
+    return fail(MOECA_E_INVAL, "the layer's experts are not quantised (moeca_layer_set_quant)");
+  if (up == nullptr || up_scale == nullptr || down == nullptr || down_scale == nullptr)
+    return fail(MOECA_E_INVAL, "the shared experts' elements and scales are required");
+  if (!aligned16(up) || !aligned16(up_scale) || !aligned16(down) || !aligned16(down_scale))
+    return fail(MOECA_E_INVAL, "shared weights must be 16-byte aligned");
+  L->qw.up_sh = up;
+  L->qw.up_sh_s = up_scale;
+  L->qw.down_sh = down;
+  L->qw.down_sh_s = down_scale;
   return MOECA_OK;
 }
 
@@ -299,8 +414,24 @@ int moeca_bind_attention(moeca_layer* L, const void* attn_in, void* attn_cache) 
     return fail(MOECA_E_INVAL, "attn_in and attn_cache must both be set or both be NULL");
   if (!aligned16(attn_in) || !aligned16(attn_cache))
     return fail(MOECA_E_INVAL, "attention buffers must be 16-byte aligned");
+  if (L->shape.cache8 && attn_in != nullptr)
+    return fail(MOECA_E_INVAL, "the layer's cache is quantised: moeca_bind_attention_quant");
   L->attn_in = attn_in;
   L->attn_cache = attn_cache;
+  return MOECA_OK;
+}
+
+int moeca_bind_attention_quant(moeca_layer* L, const void* attn_in, void* q, void* scale) {
+  if (L == nullptr) return fail(MOECA_E_INVAL, "layer is NULL");
+  if (!L->shape.cache8)
+    return fail(MOECA_E_INVAL, "the layer's cache is not quantised: moeca_bind_attention");
+  if ((attn_in == nullptr) != (q == nullptr) || (attn_in == nullptr) != (scale == nullptr))
+    return fail(MOECA_E_INVAL, "attn_in, q and scale must all be set or all be NULL");
+  if (!aligned16(attn_in) || !aligned16(q) || !aligned16(scale))
+    return fail(MOECA_E_INVAL, "attention buffers must be 16-byte aligned");
+  L->attn_in = attn_in;
+  L->attn_q = static_cast<uint8_t*>(q);
+  L->attn_s = static_cast<uint8_t*>(scale);
   return MOECA_OK;
 }
 
@@ -317,6 +448,7 @@ int moeca_forward_noalloc(const moeca_layer* L, const void* x, int samples, void
     return fail(MOECA_E_INVAL, "samples must be in [1, " + std::to_string(L->shape.B) + "]");
   Shape s = L->shape;
   s.B = samples;
+  s.cache8 = false;  // no cache here, quantised or not
   // with the down projection's K pieces if they fit (fp32 layers, and bf16
   // calls of few enough rows for the weight-streaming tiles)
   const bool split = !s.bf16 || s.branches() <= int64_t(moeca::kThinRows) * s.E;
@@ -328,8 +460,7 @@ int moeca_forward_noalloc(const moeca_layer* L, const void* x, int samples, void
                                    std::to_string(moeca::kNoallocScratchBytes) +
                                    " (use fewer samples per call, or moeca_step)");
   if (L->W_r == nullptr) return fail(MOECA_E_STATE, "weights are not bound");
-  if (s.S > 0 && L->W_up_sh == nullptr)
-    return fail(MOECA_E_STATE, "shared expert weights are not bound");
+  if (!shared_bound(L)) return fail(MOECA_E_STATE, "shared expert weights are not bound");
   void* base = nullptr;
   hipError_t e = moeca::noalloc_scratch(&base);
   if (e != hipSuccess)
@@ -337,7 +468,9 @@ int moeca_forward_noalloc(const moeca_layer* L, const void* x, int samples, void
   const Buffers b = map_buffers(static_cast<char*>(base), lay, nullptr);
   const moeca_policy& p = L->pol;
   const auto st = static_cast<hipStream_t>(stream);
-  moeca::FfnPlan plan = moeca::ffn_plan(s, moeca::kFullStep, s.branches(), b.part != nullptr);
+  moeca::FfnPlan plan =
+      s.experts8 ? moeca::q8_plan(s, moeca::kFullStep, s.branches())
+                 : moeca::ffn_plan(s, moeca::kFullStep, s.branches(), b.part != nullptr);
   if (b.part == nullptr) plan.split_down = 1;
   // the uncached layer: every branch recomputed, no statistic, no cache
   // metadata and no attention path (the MOECA_MODE_FULL step)
@@ -346,10 +479,8 @@ int moeca_forward_noalloc(const moeca_layer* L, const void* x, int samples, void
       (e = moeca::launch_decide(s, moeca::kSelFull, 0, p.lambda0, p.lambda1, p.lambda2, false,
                                 p.tau0, p.alpha, plan, b, st)) == hipSuccess &&
       (moeca::decide_lists(s) || (e = moeca::launch_lists(s, plan, b, st)) == hipSuccess) &&
-      (e = moeca::launch_ffn_up(s, x, L->W_up, L->W_up_sh, p.act, plan, b, st)) ==
-          hipSuccess &&
-      (e = moeca::launch_ffn_down(s, L->W_down, L->W_down_sh, plan, b, st)) ==
-          hipSuccess)
+      (e = ffn_up(L, s, x, plan, b, st)) == hipSuccess &&
+      (e = ffn_down(L, s, plan, b, st)) == hipSuccess)
     e = moeca::launch_combine(s, 0, moeca::combine_sums(s) ? plan.split_down : 1, out, nullptr,
                               nullptr, b, st);
   if (e != hipSuccess) return fail(MOECA_E_HIP, std::string("launch: ") + hipGetErrorString(e));
@@ -362,10 +493,7 @@ namespace moeca {
 
 int set_error(int code, const std::string& msg) { return fail(code, msg); }
 
-size_t layer_mid_bytes(const moeca_layer* L) {
-  const Shape& s = L->shape;
-  return size_t(s.mid_rows()) * s.d_ff * s.act_bytes();
-}
+size_t layer_mid_bytes(const moeca_layer* L) { return mid_bytes(L->shape); }
 
 void layer_keep_mid_outside(moeca_layer* L) {
   L->mid_outside = true;
@@ -397,8 +525,7 @@ int layer_step(moeca_layer* L, const void* x_t, const void* x_ffn, int t, void* 
   if (L->ws == nullptr) return fail(MOECA_E_STATE, "workspace is not bound");
   if (L->mid_outside && L->external_mid == nullptr)
     return fail(MOECA_E_STATE, "the FFN intermediate is not bound");
-  if (L->shape.S > 0 && L->W_up_sh == nullptr)
-    return fail(MOECA_E_STATE, "shared expert weights are not bound");
+  if (!shared_bound(L)) return fail(MOECA_E_STATE, "shared expert weights are not bound");
   const Shape& s = L->shape;
   const moeca_policy& p = L->pol;
   const bool uncached = p.mode == MOECA_MODE_FULL;
@@ -470,7 +597,8 @@ int layer_step(moeca_layer* L, const void* x_t, const void* x_ffn, int t, void* 
   // projection's sums are the same in any tiling.)
   const bool pieces = b.part != nullptr &&
                       !(L->mid_outside && kind != moeca::kRatioStep);
-  const moeca::FfnPlan plan = moeca::ffn_plan(s, kind, rows, pieces);
+  const moeca::FfnPlan plan = s.experts8 ? moeca::q8_plan(s, kind, rows)
+                                         : moeca::ffn_plan(s, kind, rows, pieces);
   arm();
   if (!check(moeca::launch_decide(s, sel, budget, p.lambda0, p.lambda1, p.lambda2, !uncached, p.tau0,
                                   p.alpha, plan, b, st),
@@ -484,15 +612,16 @@ int layer_step(moeca_layer* L, const void* x_t, const void* x_ffn, int t, void* 
     if (rc != MOECA_OK) return rc;
   }
   arm();
-  if (!check(moeca::launch_ffn_up(s, x_ffn, L->W_up, L->W_up_sh, p.act, plan, b, st), "ffn up"))
+  if (!check(ffn_up(L, s, x_ffn, plan, b, st), "ffn up"))
     return MOECA_E_HIP;
   arm();
-  if (!check(moeca::launch_ffn_down(s, L->W_down, L->W_down_sh, plan, b, st), "ffn down"))
+  if (!check(ffn_down(L, s, plan, b, st), "ffn down"))
     return MOECA_E_HIP;
   arm();
-  if (!check(moeca::launch_combine(s, uncached ? 0 : 1,
-                                   moeca::combine_sums(s) ? plan.split_down : 1, out, L->attn_in,
-                                   L->attn_cache, b, st),
+  if (!check(s.cache8 ? moeca::launch_combine_q8(s, out, L->attn_in, L->attn_q, L->attn_s, b, st)
+                      : moeca::launch_combine(s, uncached ? 0 : 1,
+                                              moeca::combine_sums(s) ? plan.split_down : 1, out,
+                                              L->attn_in, L->attn_cache, b, st),
              "combine"))
     return MOECA_E_HIP;
   if (timed) ++L->timed_steps;

@@ -1,0 +1,320 @@
+// 8-bit rows: quantising them as they are written into slots, reading them
+// back, and the combine of a layer whose cache is held that way.
+//
+// All three move bytes: a row of K elements is 2 K (bf16) or 4 K (fp32) bytes
+// on one side and K + K / 128 on the other.  One wavefront per row, eight
+// elements a lane, so that a block of 128 is one 16-lane row of the wave and
+// its largest magnitude four DPP steps; every element is loaded once and kept
+// in registers between the maximum and the conversion.
+#include <algorithm>
+
+#include "common.h"
+#include "internal.h"
+#include "q8.h"
+
+#pragma clang fp contract(off)
+
+namespace moeca {
+namespace {
+
+constexpr int kRowWaves = 4;
+constexpr int kMaxRowBlocks = 1 << 20;  // grid bound; rows beyond it by a stride
+
+// q[slot[r]], s[slot[r]], norm[slot[r]] = src row r; a slot outside [0, slots)
+// leaves its row out.  The last block's elements past K are zeros.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(kRowWaves * kWave) void quant_rows_kernel(
+    const T* __restrict__ src, int64_t rows, int K, int64_t ld, const int32_t* __restrict__ slot,
+    int64_t slots, uint8_t* __restrict__ q, uint8_t* __restrict__ s, float* __restrict__ norm) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int pitch = static_cast<int>(q8_pitch(K)), spitch = static_cast<int>(q8_spitch(K));
+  for (int64_t r = int64_t(blockIdx.x) * kRowWaves + threadIdx.x / kWave; r < rows;
+       r += int64_t(gridDim.x) * kRowWaves) {
+    const int64_t to = slot != nullptr ? slot[r] : r;
+    if (to < 0 || to >= slots) continue;  // uniform across the wave
+    const T* const row = src + r * ld;
+    uint8_t* const qr = q + to * pitch;
+    uint8_t* const sr = s + to * spitch;
+    double ss = 0.0;
+    for (int c = lane * 8; c < pitch; c += 8 * kWave) {  // whole 16-lane rows in or out
+      float v[8];
+      load8<T, VEC>(row + c, K - c, v);
+      int byte;
+      const uint2 p = q8_quant8(v, byte);
+      *reinterpret_cast<uint2*>(qr + c) = p;
+      if ((lane & 15) == 0) sr[c / kBlk] = static_cast<uint8_t>(byte);
+      if (norm != nullptr) ss += q8_square8(p, byte);
+    }
+    if (norm != nullptr) {
+      ss = wave_sum_f64(ss);
+      if (lane == 0) norm[to] = static_cast<float>(sqrt(ss));
+    }
+  }
+}
+
+// dst row r = the values of row slot[r]; a slot outside [0, slots) gives zeros.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(kRowWaves * kWave) void dequant_rows_kernel(
+    const uint8_t* __restrict__ q, const uint8_t* __restrict__ s, int64_t slots, int K,
+    const int32_t* __restrict__ slot, int64_t rows, T* __restrict__ dst, int64_t ld) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int pitch = static_cast<int>(q8_pitch(K)), spitch = static_cast<int>(q8_spitch(K));
+  for (int64_t r = int64_t(blockIdx.x) * kRowWaves + threadIdx.x / kWave; r < rows;
+       r += int64_t(gridDim.x) * kRowWaves) {
+    const int64_t at = slot != nullptr ? slot[r] : r;
+    const bool in = at >= 0 && at < slots;
+    for (int c = lane * 8; c < K; c += 8 * kWave) {
+      float v[8];
+      if (in) {
+        const uint2 p = *reinterpret_cast<const uint2*>(q + at * pitch + c);
+        const float two = q8_two(s[at * spitch + c / kBlk]);
+        q8_unpack4(p.x, v);
+        q8_unpack4(p.y, v + 4);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] *= two;
+      } else {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = 0.0f;
+      }
+      store8<T, VEC>(dst + r * ld + c, K - c, v);
+    }
+  }
+}
+
+// Weights [count][N][K] (dense) to q [count][N][pitch], s [count][ceil(N / 128)]
+// [spitch]: a block per 128 x 128 of a matrix, its 64 elements a thread kept in
+// registers between the maximum and the conversion.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void quant_matrix_kernel(const T* __restrict__ W, int N, int K,
+                                                           uint8_t* __restrict__ q,
+                                                           uint8_t* __restrict__ s) {
+  __shared__ float s_top[4];
+  const int pitch = static_cast<int>(q8_pitch(K)), spitch = static_cast<int>(q8_spitch(K));
+  const int nb = (N + kBlk - 1) / kBlk;
+  const int kb = blockIdx.x, n0 = blockIdx.y * kBlk;
+  const int64_t i = blockIdx.z;
+  const int tid = threadIdx.x;
+  const int c = kb * kBlk + (tid & 15) * 8;
+  float v[8][8];
+  float top = 0.0f;
+#pragma unroll
+  for (int h = 0; h < 8; ++h) {
+    const int n = n0 + (tid >> 4) + 16 * h;
+    if (n < N) {
+      load8<T, VEC>(W + (i * N + n) * K + c, K - c, v[h]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[h][u] = 0.0f;
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) top = fmaxf(top, q8_mag(v[h][u]));
+  }
+  top = row_max_f32(top);
+  top = fmaxf(top, __shfl_xor(top, 16, kWave));
+  top = fmaxf(top, __shfl_xor(top, 32, kWave));
+  if ((tid & (kWave - 1)) == 0) s_top[tid / kWave] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+  const int byte = q8_scale_byte(top);
+  const float inv = q8_inv(byte);
+  if (tid == 0) s[(i * nb + blockIdx.y) * spitch + kb] = static_cast<uint8_t>(byte);
+#pragma unroll
+  for (int h = 0; h < 8; ++h) {
+    const int n = n0 + (tid >> 4) + 16 * h;
+    if (n >= N) continue;
+    const float* x = v[h];
+    *reinterpret_cast<uint2*>(q + (i * N + n) * pitch + c) =
+        make_uint2(q8_pack4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv),
+                   q8_pack4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv));
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Combine of a layer whose cache is held in 8 bits (Sec. 4.1):
+//
+//   y_i = sum_s h_s + sum_p f32(w_p * hhat_p)
+//
+// as in combine.hip, with hhat_p the row that the down projection just left in
+// `fresh` (list order, activation type) for a recomputed branch, unrounded by
+// the cache, and the stored value q 2^e of slot sigma(p) for a reused one.
+// A recomputed row is quantised into its slot on the way, with the norm of
+// what is stored; a synchronised token's attention feature goes into its row of
+// the 8-bit attention cache.
+// ---------------------------------------------------------------------------
+template <typename T, int KMAX>
+__global__ __launch_bounds__(kRowWaves * kWave) void combine_q8_kernel(
+    const float* __restrict__ w_t, const int32_t* __restrict__ e_t,
+    const int32_t* __restrict__ sigma, const uint8_t* __restrict__ mask,
+    const uint8_t* __restrict__ sync, const int32_t* __restrict__ pos,
+    const T* __restrict__ fresh, uint8_t* __restrict__ h_c, uint8_t* __restrict__ s_c,
+    int32_t* __restrict__ e_c, float* __restrict__ w_c, float* __restrict__ n_c,
+    T* __restrict__ out, const T* __restrict__ attn_in, uint8_t* __restrict__ attn_q,
+    uint8_t* __restrict__ attn_s, const T* __restrict__ h_sh, int S, int64_t T_tokens, int d,
+    int k) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int64_t t = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x)) *
+                        int64_t(kRowWaves) +
+                    __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+  if (t >= T_tokens) return;
+  const int pitch = static_cast<int>(q8_pitch(d)), spitch = static_cast<int>(q8_spitch(d));
+  float wp[KMAX];
+  int slot[KMAX], from[KMAX];  // from: row of `fresh`, -1 for a reused branch
+  double ss[KMAX];
+#pragma unroll
+  for (int p = 0; p < KMAX; ++p) {
+    wp[p] = 0.0f;
+    slot[p] = 0;
+    from[p] = -1;
+    ss[p] = 0.0;
+    if (p < k) {
+      const int64_t f = t * k + p;
+      wp[p] = w_t[f];
+      slot[p] = sigma[f];
+      from[p] = mask[f] != 0 ? pos[f] : -1;
+    }
+  }
+  const bool syn = attn_in != nullptr && sync[t] != 0;
+
+  for (int c = lane * 8; c < pitch; c += 8 * kWave) {
+    const int n = d - c;  // d is a multiple of 64: eight or none
+    float acc[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) acc[u] = 0.0f;
+    for (int sh = 0; sh < S; ++sh) {
+      float h[8];
+      load8<T, true>(h_sh + (sh * T_tokens + t) * d + c, n, h);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) acc[u] = __fadd_rn(acc[u], h[u]);
+    }
+#pragma unroll
+    for (int p = 0; p < KMAX; ++p) {
+      if (p >= k) continue;
+      float h[8];
+      uint8_t* const qr = h_c + (t * k + slot[p]) * pitch + c;
+      uint8_t* const sr = s_c + (t * k + slot[p]) * spitch + c / kBlk;
+      if (from[p] >= 0) {  // uniform across the wave
+        load8<T, true>(fresh + int64_t(from[p]) * d + c, n, h);
+        int byte;
+        const uint2 q = q8_quant8(h, byte);
+        *reinterpret_cast<uint2*>(qr) = q;
+        if ((lane & 15) == 0) *sr = static_cast<uint8_t>(byte);
+        ss[p] += q8_square8(q, byte);
+      } else {
+        const uint2 q = *reinterpret_cast<const uint2*>(qr);
+        const float two = q8_two(*sr);
+        q8_unpack4(q.x, h);
+        q8_unpack4(q.y, h + 4);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) h[u] = __fmul_rn(h[u], two);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) acc[u] = __fadd_rn(acc[u], __fmul_rn(wp[p], h[u]));
+    }
+    if (n > 0) store8<T, true>(out + t * d + c, n, acc);
+    if (syn) {
+      float a[8];
+      load8<T, true>(attn_in + t * d + c, n, a);
+      int byte;
+      *reinterpret_cast<uint2*>(attn_q + t * pitch + c) = q8_quant8(a, byte);
+      if ((lane & 15) == 0) attn_s[t * spitch + c / kBlk] = static_cast<uint8_t>(byte);
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < KMAX; ++p) {
+    if (p >= k || from[p] < 0) continue;  // uniform across the wave
+    const double sq = wave_sum_f64(ss[p]);
+    if (lane == 0) {
+      const int64_t c = t * k + slot[p];
+      n_c[c] = static_cast<float>(sqrt(sq));
+      e_c[c] = e_t[t * k + p];
+      w_c[c] = wp[p];
+    }
+  }
+}
+
+bool vec_rows(const void* p, int64_t ld, size_t elem) {
+  return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * elem % 16 == 0;
+}
+
+unsigned row_blocks(int64_t rows) {
+  return static_cast<unsigned>(
+      std::min<int64_t>((rows + kRowWaves - 1) / kRowWaves, kMaxRowBlocks));
+}
+
+}  // namespace
+
+hipError_t launch_quant_rows(const void* src, bool bf16, int64_t rows, int K, int64_t ld,
+                             const int32_t* slot, int64_t slots, uint8_t* q, uint8_t* s,
+                             float* norm, hipStream_t st) {
+  const dim3 grid(row_blocks(rows)), block(kRowWaves * kWave);
+#define MOECA_QROWS(T, V)                                                                        \
+  launch_kernel(&quant_rows_kernel<T, V>, grid, block, 0, st, static_cast<const T*>(src), rows, \
+                K, ld, slot, slots, q, s, norm)
+  if (bf16) {
+    if (vec_rows(src, ld, 2)) MOECA_QROWS(uint16_t, true);
+    else MOECA_QROWS(uint16_t, false);
+  } else {
+    if (vec_rows(src, ld, 4)) MOECA_QROWS(float, true);
+    else MOECA_QROWS(float, false);
+  }
+#undef MOECA_QROWS
+  return hipGetLastError();
+}
+
+hipError_t launch_dequant_rows(const uint8_t* q, const uint8_t* s, int64_t slots, int K,
+                               const int32_t* slot, int64_t rows, void* dst, bool bf16,
+                               int64_t ld, hipStream_t st) {
+  const dim3 grid(row_blocks(rows)), block(kRowWaves * kWave);
+#define MOECA_DROWS(T, V)                                                                   \
+  launch_kernel(&dequant_rows_kernel<T, V>, grid, block, 0, st, q, s, slots, K, slot, rows, \
+                static_cast<T*>(dst), ld)
+  if (bf16) {
+    if (vec_rows(dst, ld, 2)) MOECA_DROWS(uint16_t, true);
+    else MOECA_DROWS(uint16_t, false);
+  } else {
+    if (vec_rows(dst, ld, 4)) MOECA_DROWS(float, true);
+    else MOECA_DROWS(float, false);
+  }
+#undef MOECA_DROWS
+  return hipGetLastError();
+}
+
+hipError_t launch_quant_matrix(const void* W, bool bf16, int count, int N, int K, uint8_t* q,
+                               uint8_t* s, hipStream_t st) {
+  const dim3 grid(static_cast<unsigned>(q8_pitch(K) / kBlk),
+                  static_cast<unsigned>((N + kBlk - 1) / kBlk), static_cast<unsigned>(count));
+#define MOECA_QMAT(T, V)                                                                       \
+  launch_kernel(&quant_matrix_kernel<T, V>, grid, dim3(256), 0, st, static_cast<const T*>(W), N, \
+                K, q, s)
+  if (bf16) {
+    if (vec_rows(W, K, 2)) MOECA_QMAT(uint16_t, true);
+    else MOECA_QMAT(uint16_t, false);
+  } else {
+    if (vec_rows(W, K, 4)) MOECA_QMAT(float, true);
+    else MOECA_QMAT(float, false);
+  }
+#undef MOECA_QMAT
+  return hipGetLastError();
+}
+
+hipError_t launch_combine_q8(const Shape& s, void* out, const void* attn_in, uint8_t* attn_q,
+                             uint8_t* attn_s, const Buffers& b, hipStream_t st) {
+  const dim3 grid(static_cast<unsigned>((s.tokens() + kRowWaves - 1) / kRowWaves));
+  const dim3 block(kRowWaves * kWave);
+#define MOECA_CQ8(T, KM)                                                                         \
+  launch_kernel(&combine_q8_kernel<T, KM>, grid, block, 0, st, b.w_t, b.e_t, b.sigma, b.mask,    \
+                b.sync, b.pos, static_cast<const T*>(b.fresh), static_cast<uint8_t*>(b.h_c),     \
+                b.s_c, b.e_c, b.w_c, b.n_c, static_cast<T*>(out), static_cast<const T*>(attn_in), \
+                attn_q, attn_s, static_cast<const T*>(b.h_sh), s.S, s.tokens(), s.d, s.k)
+  if (s.bf16) {
+    if (s.k <= 2) MOECA_CQ8(uint16_t, 2);
+    else MOECA_CQ8(uint16_t, 8);
+  } else {
+    if (s.k <= 2) MOECA_CQ8(float, 2);
+    else MOECA_CQ8(float, 8);
+  }
+#undef MOECA_CQ8
+  return hipGetLastError();
+}
+
+}  // namespace moeca

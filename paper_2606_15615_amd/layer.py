@@ -39,8 +39,13 @@ class MoecaLayer:
     def __init__(self, d, E, k, d_ff, *, batch, tokens, mode=_lib.MOECA_MODE_THRESHOLD,
                  ratio=0.3, tau0=0.80, alpha=0.6, beta=0.65, lambda1=1.0, lambda2=1.0,
                  lambda0=1.0, refresh_cycle=4, norm_topk=True, act="gelu_tanh", dtype="bf16",
-                 n_shared=0, device="cuda:0"):
+                 n_shared=0, device="cuda:0", experts=None, cache=None):
+        """experts="e4m3": expert weights (and hidden rows) in 8 bits, bound with
+        ``set_weights_quant``; cache="e4m3": the branch cache (and the attention
+        cache) in 8 bits."""
         torch = _torch()
+        if experts not in (None, "e4m3") or cache not in (None, "e4m3"):
+            raise ValueError("experts and cache are None or 'e4m3'")
         p = _lib.moeca_policy_default()
         p.mode, p.ratio, p.tau0, p.alpha, p.beta = mode, ratio, tau0, alpha, beta
         p.lambda0, p.lambda1, p.lambda2 = lambda0, lambda1, lambda2
@@ -55,7 +60,12 @@ class MoecaLayer:
         self.dtype = dtype
         self.act_np = np.uint16 if dtype == "bf16" else np.float32
         self.device = torch.device(device)
+        self.up_rows = d_ff * (2 if act == "swiglu" else 1)
+        self.experts8, self.cache8 = experts is not None, cache is not None
         self.h = _lib.moeca_layer_create(d, E, k, d_ff, p)
+        if self.experts8 or self.cache8:
+            _lib.moeca_layer_set_quant(self.h, (_lib.MOECA_QUANT_EXPERTS if self.experts8 else 0) |
+                                       (_lib.MOECA_QUANT_CACHE if self.cache8 else 0))
         nbytes = _lib.moeca_workspace_bytes(self.h)
         self._ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
         base = self._ws.data_ptr()
@@ -78,6 +88,7 @@ class MoecaLayer:
         self.h = handle
         self.workspace = workspace
         self._owned = False
+        self.experts8 = self.cache8 = False
         return self
 
     # -- binding ---------------------------------------------------------
@@ -91,7 +102,43 @@ class MoecaLayer:
         self._keep_shared = [W_up_s, W_down_s]
         _lib.moeca_layer_set_shared(self.h, W_up_s.data_ptr(), W_down_s.data_ptr())
 
+    def _mats(self, ms, n, N, K):
+        for m in ms:
+            if (m.q.ndim != 3 or m.q.shape[0] != n or (m.N, m.K) != (N, K) or
+                    m.q.device != self.device):
+                raise ValueError(f"expected {n} quantised matrices of {N} x {K} on {self.device}")
+        return [t.data_ptr() for m in ms for t in (m.q, m.scale)]
+
+    def set_weights_quant(self, W_r, b_r, up, down):
+        """``up`` and ``down``: stacks of E ``quant.QuantMatrix`` (experts="e4m3")."""
+        ptrs = (self._mats([up], self.E, self.up_rows, self.d) +
+                self._mats([down], self.E, self.d, self.d_ff))
+        _lib.moeca_layer_set_weights_quant(self.h, W_r.data_ptr(),
+                                           None if b_r is None else b_r.data_ptr(), *ptrs)
+        self._keep = [W_r, b_r, up, down]
+
+    def set_shared_quant(self, up, down):
+        ptrs = (self._mats([up], self.n_shared, self.up_rows, self.d) +
+                self._mats([down], self.n_shared, self.d, self.d_ff))
+        _lib.moeca_layer_set_shared_quant(self.h, *ptrs)
+        self._keep_shared = [up, down]
+
     def bind_attention(self, attn_in, attn_cache):
+        """``attn_cache``: a tensor like ``attn_in``, or, for cache="e4m3", a
+        ``quant.QuantRows`` of B*N rows of width d."""
+        if self.cache8 and attn_cache is not None:
+            if ((attn_cache.slots, attn_cache.K) != (self.B * self.N, self.d) or
+                    attn_cache.q.device != self.device):
+                raise ValueError(f"expected {self.B * self.N} quantised rows of width {self.d} "
+                                 f"on {self.device}")
+            _lib.moeca_bind_attention_quant(self.h, attn_in.data_ptr(), attn_cache.q.data_ptr(),
+                                            attn_cache.scale.data_ptr())
+            self._attn = (attn_in, attn_cache)
+            return
+        if self.cache8:
+            _lib.moeca_bind_attention_quant(self.h, None, None, None)
+            self._attn = None
+            return
         self._attn = (attn_in, attn_cache)
         _lib.moeca_bind_attention(self.h, None if attn_in is None else attn_in.data_ptr(),
                                   None if attn_cache is None else attn_cache.data_ptr())
@@ -110,6 +157,16 @@ class MoecaLayer:
 
     def stats(self, stream=None):
         return _lib.moeca_get_stats(self.h, self._stream(stream))
+
+    def cache_rows(self):
+        """The branch cache of a cache="e4m3" layer as a ``quant.QuantRows`` of
+        B*N*k rows (slot q of token i at row i*k + q): a view of the workspace."""
+        from . import quant
+        torch = _torch()
+        n = self.B * self.N * self.k
+        return quant.QuantRows(n, self.d, q=self.buffer("h_c").view(n, -1),
+                               scale=self.buffer("s_c").view(n, -1),
+                               norm=self.buffer("n_c").view(torch.float32))
 
     def set_valid(self, valid: bool):
         _lib.moeca_debug_set_valid(self.h, 1 if valid else 0)
@@ -134,6 +191,9 @@ class MoecaLayer:
             "sigma": (np.int32, nbr), "sync": (np.uint8, (B * N,)), "off": (np.int32, (E + 1,)),
             "list": (np.int32, nbr), "pos": (np.int32, nbr),
         }
+        if self.cache8:
+            table["h_c"] = (np.uint8, (B * N * k, _lib.moeca_quant_pitch(d)))
+            table["s_c"] = (np.uint8, (B * N * k, _lib.moeca_quant_scale_pitch(d)))
         return table[name]
 
     def buffer(self, name):

@@ -1,0 +1,207 @@
+"""8-bit rows and matrices on a GPU: e4m3 elements with a power-of-two scale for
+each block of 128 (include/moeca.h states the stored form).
+
+``QuantRows`` are rows that are quantised as they are written into slots and
+read back by slot; ``QuantMatrix`` holds one weight matrix, or a stack of them,
+with a scale per 128 x 128 block; ``linear`` multiplies rows with a matrix.
+torch provides device memory and the stream; the arithmetic runs in the
+library's kernels.  Calls run on their tensors' device, on its current stream
+unless one is given.
+"""
+from __future__ import annotations
+
+from . import _lib
+from .layer import _torch
+
+
+def _dtype(t):
+    torch = _torch()
+    if t.dtype == torch.bfloat16:
+        return _lib.MOECA_DTYPE_BF16
+    if t.dtype == torch.float32:
+        return _lib.MOECA_DTYPE_FP32
+    raise TypeError(f"rows are bfloat16 or float32, not {t.dtype}")
+
+
+def _on(device, stream):
+    """The device's guard, and the stream to enqueue on."""
+    torch = _torch()
+    s = stream if stream is not None else torch.cuda.current_stream(device)
+    return torch.cuda.device(device), s.cuda_stream
+
+
+def _rows(t, width, device, what):
+    """(pointer, rows, row stride) of a 2-d tensor of the activation type."""
+    if t.ndim != 2 or t.shape[1] != width:
+        raise ValueError(f"{what}: expected rows of width {width}, got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, expected {device}")
+    if t.shape[0] > 0 and width > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: the elements of a row must be contiguous")
+    ld = t.stride(0) if t.shape[0] > 1 else width
+    if ld < width:
+        raise ValueError(f"{what}: rows overlap (stride {ld}, width {width})")
+    return t.data_ptr() or None, t.shape[0], ld
+
+
+def _indexes(slot, rows, device):
+    if slot is None:
+        return None
+    torch = _torch()
+    if slot.dtype != torch.int32 or slot.ndim != 1 or not slot.is_contiguous():
+        raise ValueError("slots are a contiguous int32 vector")
+    if slot.device != device:
+        raise ValueError(f"slots are on {slot.device}, expected {device}")
+    if rows is not None and slot.shape[0] != rows:
+        raise ValueError(f"{slot.shape[0]} slots for {rows} rows")
+    return slot.data_ptr() or None
+
+
+def _bytes(t, shape, what):
+    """A dense 8-bit tensor of this shape, as uint8."""
+    torch = _torch()
+    if t.element_size() != 1 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what}: expected contiguous bytes of shape {tuple(shape)}, "
+                         f"got {t.dtype} {tuple(t.shape)}")
+    return t.view(torch.uint8)
+
+
+class QuantRows:
+    """``slots`` rows of width K: ``q`` [slots][pitch], ``scale`` [slots][scale pitch]
+    and, if wanted, ``norm`` [slots] (fp32, of the stored values).  New buffers
+    start as zeros."""
+
+    def __init__(self, slots, K, *, device="cuda:0", q=None, scale=None, norm=False):
+        torch = _torch()
+        self.slots, self.K = int(slots), int(K)
+        if self.slots < 0 or self.K < 1:
+            raise ValueError("slots must be >= 0 and K >= 1")
+        self.pitch, self.scale_pitch = _lib.moeca_quant_pitch(K), _lib.moeca_quant_scale_pitch(K)
+        if (q is None) != (scale is None):
+            raise ValueError("q and scale come together")
+        if q is None:
+            q = torch.zeros(self.slots, self.pitch, dtype=torch.uint8, device=device)
+            scale = torch.zeros(self.slots, self.scale_pitch, dtype=torch.uint8, device=device)
+        self.q = _bytes(q, (self.slots, self.pitch), "q")
+        self.scale = _bytes(scale, (self.slots, self.scale_pitch), "scale")
+        if norm is True:
+            norm = torch.zeros(self.slots, device=self.q.device)
+        self.norm = None if norm is None or norm is False else norm
+        if self.norm is not None and (self.norm.dtype != torch.float32 or self.norm.ndim != 1 or
+                                      self.norm.shape[0] != self.slots or
+                                      not self.norm.is_contiguous()):
+            raise ValueError("norm: expected a contiguous float32 vector, one per slot")
+        for t in (self.scale, self.norm):
+            if t is not None and t.device != self.q.device:
+                raise ValueError("q, scale and norm must be on one device")
+
+    def write(self, x, slot=None, stream=None):
+        """Quantise the rows of ``x`` [rows][K] into ``slot`` (int32, default row r into
+        slot r); a slot outside the range leaves its row out."""
+        p, rows, ld = _rows(x, self.K, self.q.device, "x")
+        at = _indexes(slot, rows, self.q.device)
+        if rows == 0:
+            return
+        dev, st = _on(self.q.device, stream)
+        with dev:
+            _lib.moeca_quant_rows(p, _dtype(x), rows, self.K, ld, at, self.slots,
+                                  self.q.data_ptr(), self.scale.data_ptr(),
+                                  None if self.norm is None else self.norm.data_ptr(), st)
+
+    def read(self, slot=None, dtype=None, out=None, stream=None):
+        """The values of rows ``slot`` (default: all), in ``out`` or a new tensor of
+        ``dtype`` (bfloat16); a slot outside the range gives zeros."""
+        torch = _torch()
+        at = _indexes(slot, None, self.q.device)
+        rows = self.slots if slot is None else slot.shape[0]
+        if out is None:
+            out = torch.empty(rows, self.K, dtype=dtype or torch.bfloat16, device=self.q.device)
+        elif dtype is not None and out.dtype != dtype:
+            raise TypeError(f"out is {out.dtype}, not {dtype}")
+        p, n, ld = _rows(out, self.K, self.q.device, "out")
+        if n != rows:
+            raise ValueError(f"out has {n} rows for {rows}")
+        if rows == 0:
+            return out
+        dev, st = _on(self.q.device, stream)
+        with dev:
+            _lib.moeca_dequant_rows(self.q.data_ptr(), self.scale.data_ptr(), self.slots, self.K,
+                                    at, rows, p, _dtype(out), ld, st)
+        return out
+
+
+class QuantMatrix:
+    """A weight matrix of N rows (out) and K inputs, or a stack of n of them: ``q``
+    [n][N][pitch], ``scale`` [n][ceil(N / 128)][scale pitch] (one matrix: without n)."""
+
+    def __init__(self, q, scale, N, K):
+        self.N, self.K = int(N), int(K)
+        lead = tuple(q.shape[:-2])
+        if len(lead) > 1:
+            raise ValueError("q has two dimensions, or three for a stack")
+        self.q = _bytes(q, lead + (self.N, _lib.moeca_quant_pitch(K)), "q")
+        self.scale = _bytes(scale, lead + (-(-self.N // 128), _lib.moeca_quant_scale_pitch(K)),
+                            "scale")
+        if self.scale.device != self.q.device:
+            raise ValueError("q and scale must be on one device")
+
+
+def quantize_matrix(W, stream=None) -> QuantMatrix:
+    """Quantise W [N][K], or a stack [n][N][K], bfloat16 or float32."""
+    torch = _torch()
+    if W.ndim not in (2, 3) or not W.is_contiguous():
+        raise ValueError("W is a contiguous [N][K] or [n][N][K] tensor")
+    N, K = W.shape[-2:]
+    lead = tuple(W.shape[:-2])
+    q = torch.empty(lead + (N, _lib.moeca_quant_pitch(K)), dtype=torch.uint8, device=W.device)
+    s = torch.zeros(lead + (-(-N // 128), _lib.moeca_quant_scale_pitch(K)), dtype=torch.uint8,
+                    device=W.device)
+    dev, st = _on(W.device, stream)
+    with dev:
+        _lib.moeca_quant_matrix(W.data_ptr(), _dtype(W), lead[0] if lead else 1, N, K,
+                                q.data_ptr(), s.data_ptr(), st)
+    return QuantMatrix(q, s, N, K)
+
+
+def linear_workspace(M, K, device="cuda:0"):
+    """A workspace for ``linear`` calls of up to M rows of width K, one at a time."""
+    torch = _torch()
+    return torch.empty(_lib.moeca_quant_linear_bytes(M, K), dtype=torch.uint8, device=device)
+
+
+def linear(x, W: QuantMatrix, bias=None, out=None, workspace=None, stream=None):
+    """x W^T (+ bias) for rows x [M][K] (bfloat16 or float32; quantised by the call)
+    and one quantised matrix; ``out`` [M][N] is of x's type.  Without a
+    ``workspace`` one is allocated for the call, which then has to run on the
+    current stream."""
+    torch = _torch()
+    if W.q.ndim != 2:
+        raise ValueError("linear takes one matrix, not a stack")
+    device = W.q.device
+    px, M, ldx = _rows(x, W.K, device, "x")
+    dt = _dtype(x)
+    if out is None:
+        out = torch.empty(M, W.N, dtype=x.dtype, device=device)
+    elif out.dtype != x.dtype:
+        raise TypeError(f"out is {out.dtype}, x {x.dtype}")
+    po, n, ldo = _rows(out, W.N, device, "out")
+    if n != M:
+        raise ValueError(f"out has {n} rows, x {M}")
+    if bias is not None and (bias.dtype != torch.float32 or tuple(bias.shape) != (W.N,) or
+                             not bias.is_contiguous() or bias.device != device):
+        raise ValueError(f"bias: expected a contiguous float32 vector of {W.N} on {device}")
+    if M == 0:
+        return out
+    if workspace is None:
+        if stream is not None and stream != torch.cuda.current_stream(device):
+            raise ValueError("a call on another stream needs a workspace of its own")
+        workspace = linear_workspace(M, W.K, device)
+    elif workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: expected contiguous bytes on {device}")
+    dev, st = _on(device, stream)
+    with dev:
+        _lib.moeca_quant_linear(px, dt, M, W.K, ldx, W.q.data_ptr(), W.scale.data_ptr(), W.N,
+                                None if bias is None else bias.data_ptr(), po, ldo,
+                                workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                st)
+    return out
