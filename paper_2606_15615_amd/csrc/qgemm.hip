@@ -32,6 +32,7 @@
 // hidden rows are never held in more than 8 bits, and the activation's value
 // is rounded once, from fp32.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "gemm.h"
@@ -55,6 +56,8 @@ struct QArgs {
   const int32_t *off, *tile_off, *list, *row_dst;
   int E, G, k;     // routed groups, all groups, branches a token
   int M;           // dense: rows
+  const int32_t* tm;  // rows of a 256-column tile, at most (from the lists kernel)
+  int dense_tm;       // the same of a dense product
   int pitch, spitch;
   int Nout;        // weight rows of a group
   int64_t ldo;     // elements of an output row (down, dense)
@@ -115,6 +118,12 @@ __device__ __forceinline__ f32x4_t mfma_q8(const Piece<true>& w, const Piece<tru
   return c;
 }
 
+typedef __attribute__((ext_vector_type(2))) float f32x2_q;
+// Two fp32 -> two bf16 (hardware round to nearest even), packed in 4 bytes.
+__device__ __forceinline__ uint32_t pack2_bf16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_q{a, b}, bf16x2_q));
+}
+
 // Four consecutive outputs of a row from column c on; whole: all four exist and
 // the address is a multiple of their size.
 template <typename T>
@@ -135,34 +144,103 @@ __device__ __forceinline__ void store4(T* p, f32x4_t v, int n, bool whole) {
 }
 
 // ---------------------------------------------------------------------------
-// 128-row tiles, 128 columns (gated: 256 weight rows, 128 hidden columns, so
-// that a tile has whole blocks of the hidden rows).  256 threads as 2 x 2
-// waves, k-tile 128, LDS double buffered in rows of 144 bytes (no two of the
-// 16 rows of a read share a bank), the next k-tile loaded into registers
-// while this one is multiplied.
+// What the tiles' epilogues share.  A wave has JT x IT accumulator tiles, tile j
+// of columns and i of rows; the lane holds columns c .. c + 3 of row (lane & 15),
+// c = (first column of tile j) + 4 (lane / 16).
 // ---------------------------------------------------------------------------
-constexpr int kQTM = 128;
-constexpr int kQThreads = 256;
-constexpr int kQRow = kBlk + 16;
+
+// The activation of an accumulator tile in place (gated: the two hidden values
+// in v[0], v[1]), zeros in hidden columns past the width (their weight rows are
+// clamped), and the largest magnitude.
+template <int ACT>
+__device__ __forceinline__ float hidden4(f32x4_t& v, int c, int Nout) {
+  if constexpr (ACT == kActSwiglu) {
+    v[0] = c < Nout ? silu_f(v[0]) * v[1] : 0.0f;
+    v[1] = c + 2 < Nout ? silu_f(v[2]) * v[3] : 0.0f;
+    return fmaxf(q8_mag(v[0]), q8_mag(v[1]));
+  } else {
+    float top = 0.0f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      v[u] = c + u < Nout ? act_fn<ACT>(v[u]) : 0.0f;
+      top = fmaxf(top, q8_mag(v[u]));
+    }
+    return top;
+  }
+}
+
+// Quantised hidden values of a tile into their row, from hidden column c (gated:
+// c / 2) on.
+template <int ACT>
+__device__ __forceinline__ void store_hidden4(uint8_t* row, int c, f32x4_t v, float inv) {
+  if constexpr (ACT == kActSwiglu)
+    *reinterpret_cast<uint16_t*>(row + c / 2) =
+        static_cast<uint16_t>(q8_pack4(v[0] * inv, v[1] * inv, 0.0f, 0.0f));
+  else
+    *reinterpret_cast<uint32_t*>(row + c) =
+        q8_pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+}
+
+template <typename T>
+__device__ __forceinline__ void store_out4(const QArgs& a, T* row, int c, f32x4_t v, bool vec) {
+  if (a.bias != nullptr) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (c + u < a.Nout) v[u] += a.bias[c + u];
+  }
+  store4(row + c, v, a.Nout - c, vec && c + 4 <= a.Nout);
+}
+
+// Source and destination row of row r of a tile (`rows` rows from r0 on).
+template <int KIND>
+__device__ __forceinline__ void tile_row(const QArgs& a, int e, int r0, int rows, int r, int& src,
+                                         int& dst) {
+  if constexpr (KIND == kDense) {
+    src = r0 + (r < rows ? r : 0);
+    dst = r < rows ? r0 + r : -1;
+  } else {
+    group_row<KIND>(e, a.E, r0, rows, r, a.k, a.off, a.list, a.row_dst, src, dst);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// 128 x 256 tiles: 8 waves (2 x 4) of 64 rows x 64 columns, 4 x 4 tiles of
+// 16 x 16 each (weights the A operand).  A k-tile is 128 bytes of every row, one
+// block; three of them (48 KB each) are in LDS or on their way, brought by direct
+// global -> LDS loads in the XOR-swizzled order of the bf16 kernels: position p
+// of row r holds 16-byte chunk p ^ ((r >> 1) & 7).  The scales come the same
+// way, 16 bytes (16 k-tiles) of each row at a time, into one of two buffers; a
+// k-tile's are read as bytes.  An up projection's block of 128 hidden columns
+// lies with two waves of a row (gated: four), which exchange their largest
+// magnitudes through LDS.  Persistent, one block per CU; the next tile's first
+// loads start before this tile's epilogue.
+// ---------------------------------------------------------------------------
+constexpr int kMidTM = 128;
+constexpr int kMidTN = 256;
+constexpr int kMidWaves = 8;
+constexpr int kMidThreads = kMidWaves * kWave;
+constexpr int kMidStages = 3;
+constexpr int kMidTileX = kMidTM * kBlk;               // bytes
+constexpr int kMidStage = kMidTileX + kMidTN * kBlk;   // 48 KB
+constexpr int kMidLoadsX = kMidTM / 8 / kMidWaves;     // 2 per wave and stage
+constexpr int kMidLoadsW = kMidTN / 8 / kMidWaves;     // 4
+constexpr int kMidScales = (kMidTM + 2) * 16;          // bytes of a scale buffer: rows, two blocks
 
 template <int KIND, int ACT, typename T, bool EXACT>
-__global__ __launch_bounds__(kQThreads, 1) void qgemm_kernel(QArgs a) {
+__global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
   constexpr bool kGated = ACT == kActSwiglu;
-  constexpr int TN = kGated ? 256 : 128;
-  constexpr int WN = TN / 2;          // wave columns
-  constexpr int FM = 4, FN = WN / 16;  // 16 x 16 tiles of a wave
-  constexpr int LA = kQTM / 32, LB = TN / 32;
-  __shared__ __attribute__((aligned(16))) uint8_t Xl[2][kQTM * kQRow];
-  __shared__ __attribute__((aligned(16))) uint8_t Wl[2][TN * kQRow];
-  __shared__ int s_src[kQTM], s_dst[kQTM];
-  __shared__ float s_top[2][kQTM];
+  constexpr int FM = 4, FN = 4;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kMidStages * kMidStage];
+  __shared__ __attribute__((aligned(16))) uint8_t s_sc[2][kMidScales];
+  __shared__ int s_src[kMidTM], s_dst[kMidTM];
+  __shared__ float s_top[KIND == kUp ? 4 : 1][kMidTM];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
-  const int wv = tid >> 6;
-  const int wm = wv >> 1, wn = wv & 1;
-  const int nt = (a.Nout + TN - 1) / TN;
-  const int total = KIND == kDense ? (a.M + kQTM - 1) / kQTM * nt : a.tile_off[a.G];
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wv >> 2, wn = wv & 3;
+  const int nt = (a.Nout + kMidTN - 1) / kMidTN;
+  const int total = KIND == kDense ? (a.M + kMidTM - 1) / kMidTM * nt : a.tile_off[a.G];
   const int per = (total + kXcds - 1) / kXcds;
   const int lo = (blockIdx.x % kXcds) * per;
   const int hi = min(total, lo + per);
@@ -174,194 +252,690 @@ __global__ __launch_bounds__(kQThreads, 1) void qgemm_kernel(QArgs a) {
   }
   const int KT = a.pitch / kBlk;
   const int nbw = (a.Nout + kBlk - 1) / kBlk;
-  const int lrow = tid >> 3, lcol = (tid & 7) * 16;
+  const int chunk = (lane & 7) ^ (4 * (wv & 1) + (lane >> 4));
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(lds) + wv * 1024);
+  const uint32_t sc0 = __builtin_amdgcn_readfirstlane(lds_addr(&s_sc[0][0]) + wv * 1024);
 
-  for (int L = lo + static_cast<int>(blockIdx.x) / kXcds; L < hi; L += stride) {
-    int e = 0, e_base = 0, o0 = 0, cnt = a.M;
+  struct Tile {
+    int e, r0, rows, n0;
+  };
+  auto tile = [&](int L) __attribute__((always_inline)) {
+    Tile t;
+    int e_base = 0, o0 = 0, cnt = a.M;
+    t.e = 0;
     if constexpr (KIND != kDense) {
-      e = tile_group(L, toff0, toff1, e_base);
-      o0 = a.off[e];
-      cnt = a.off[e + 1] - o0;
+      t.e = tile_group(L, toff0, toff1, e_base);
+      o0 = a.off[t.e];
+      cnt = a.off[t.e + 1] - o0;
     }
-    const int mt = (cnt + kQTM - 1) / kQTM;
+    const int mt = (cnt + kMidTM - 1) / kMidTM;
     const int local = L - e_base;
     const int m = local % mt;
-    const int r0 = o0 + m * kQTM;
-    const int rows = min(kQTM, cnt - m * kQTM);
-    const int n0 = (local / mt) * TN;
-    const bool routed = KIND == kDense || e < a.E;
-    const int64_t g = routed ? e : e - a.E;
-    const uint8_t* const Wg = (routed ? a.W : a.Wsh) + g * a.Nout * a.pitch;
-    const uint8_t* const Wsg = (routed ? a.Ws : a.Wssh) + g * nbw * a.spitch;
+    t.e = __builtin_amdgcn_readfirstlane(t.e);
+    t.r0 = __builtin_amdgcn_readfirstlane(o0 + m * kMidTM);
+    t.rows = __builtin_amdgcn_readfirstlane(min(kMidTM, cnt - m * kMidTM));
+    t.n0 = __builtin_amdgcn_readfirstlane((local / mt) * kMidTN);
+    return t;
+  };
 
-    for (int r = tid; r < kQTM; r += kQThreads) {
-      if constexpr (KIND == kDense) {
-        s_src[r] = r < rows ? r0 + r : r0;
-        s_dst[r] = r < rows ? r0 + r : -1;
-      } else {
-        group_row<KIND>(e, a.E, r0, rows, r, a.k, a.off, a.list, a.row_dst, s_src[r], s_dst[r]);
-      }
+  const uint8_t *gx[kMidLoadsX], *gw[kMidLoadsW], *gs = nullptr;
+  auto start = [&](const Tile& t, int src, int dst) __attribute__((always_inline)) {
+    if (tid < kMidTM) {
+      s_src[tid] = src;
+      s_dst[tid] = dst;
     }
     __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kMidLoadsX; ++u)
+      gx[u] = a.X + int64_t(s_src[8 * (wv + kMidWaves * u) + (lane >> 3)]) * a.pitch + chunk * 16;
+    const bool routed = KIND == kDense || t.e < a.E;
+    const int64_t g = routed ? t.e : t.e - a.E;
+    const uint8_t* const W = (routed ? a.W : a.Wsh) + g * a.Nout * a.pitch;
+#pragma unroll
+    for (int u = 0; u < kMidLoadsW; ++u) {
+      const int n = min(t.n0 + 8 * (wv + kMidWaves * u) + (lane >> 3), a.Nout - 1);
+      gw[u] = W + int64_t(n) * a.pitch + chunk * 16;
+    }
+    // scales: waves 0 and 1 the rows', two lanes of wave 2 the weight blocks'
+    if (wv < 2)
+      gs = a.Xs + int64_t(s_src[64 * wv + lane]) * a.spitch;
+    else if (wv == 2)
+      gs = (routed ? a.Ws : a.Wssh) +
+           (g * nbw + min(t.n0 / kBlk + (lane & 1), nbw - 1)) * a.spitch;
+  };
+  auto issue = [&](int kt, int st) __attribute__((always_inline)) {
+    const uint32_t base = lds0 + st * kMidStage;
+#pragma unroll
+    for (int u = 0; u < kMidLoadsX; ++u)
+      dma16(reinterpret_cast<const uint16_t*>(gx[u] + int64_t(kt) * kBlk),
+            base + u * kMidWaves * 1024);
+#pragma unroll
+    for (int u = 0; u < kMidLoadsW; ++u)
+      dma16(reinterpret_cast<const uint16_t*>(gw[u] + int64_t(kt) * kBlk),
+            base + kMidTileX + u * kMidWaves * 1024);
+  };
+  auto issue_scales = [&](int c) __attribute__((always_inline)) {
+    // the LDS address is the wave's: say so inside the lanes' branch too
+    if (wv < 2 || (wv == 2 && lane < 2))
+      dma16(reinterpret_cast<const uint16_t*>(gs + c * 16),
+            __builtin_amdgcn_readfirstlane(sc0 + (c & 1) * kMidScales));
+  };
+  // the first two k-tiles and 16 k-tiles' scales of a tile
+  auto begin = [&]() __attribute__((always_inline)) {
+    issue_scales(0);
+    issue(0, 0);
+    if (KT > 1) issue(1, 1);
+  };
 
-    const uint8_t *xp[LA], *wp[LB], *xsp[FM];
-#pragma unroll
-    for (int i = 0; i < LA; ++i) xp[i] = a.X + int64_t(s_src[lrow + 32 * i]) * a.pitch + lcol;
-#pragma unroll
-    for (int i = 0; i < LB; ++i)
-      wp[i] = Wg + int64_t(min(n0 + lrow + 32 * i, a.Nout - 1)) * a.pitch + lcol;
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-      xsp[i] = a.Xs + int64_t(s_src[wm * 64 + i * 16 + (lane & 15)]) * a.spitch;
-    const uint8_t* const wsp = Wsg + int64_t(min((n0 + wn * WN) / kBlk, nbw - 1)) * a.spitch;
+  int L = lo + static_cast<int>(blockIdx.x) / kXcds;
+  if (L >= hi) return;
+  Tile cur = tile(L);
+  {
+    int src = 0, dst = -1;
+    if (tid < kMidTM) tile_row<KIND>(a, cur.e, cur.r0, cur.rows, tid, src, dst);
+    start(cur, src, dst);
+  }
+  begin();
+  const uint32_t fr = (lane & 15) * kBlk + (((lane >> 4) ^ ((lane >> 1) & 7)) * 16);
 
+  for (;;) {
+    const int Ln = L + stride;
+    const bool has_next = Ln < hi;
+    Tile nxt = cur;
+    int nsrc = 0, ndst = -1;
+    if (has_next) {
+      nxt = tile(Ln);
+      if (tid < kMidTM) tile_row<KIND>(a, nxt.e, nxt.r0, nxt.rows, tid, nsrc, ndst);
+    }
     f32x4_t acc[FN][FM];
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
       for (int i = 0; i < FM; ++i) acc[j][i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-
-    u32x4_t R[LA + LB];
-    int sx[FM], sw, sxn[FM], swn;
-    auto gload = [&](int kt) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < LA; ++i) R[i] = *reinterpret_cast<const u32x4_t*>(xp[i] + kt * kBlk);
-#pragma unroll
-      for (int i = 0; i < LB; ++i)
-        R[LA + i] = *reinterpret_cast<const u32x4_t*>(wp[i] + kt * kBlk);
-#pragma unroll
-      for (int i = 0; i < FM; ++i) sxn[i] = xsp[i][kt];
-      swn = wsp[kt];
-    };
-    auto lstore = [&](int b) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < LA; ++i)
-        *reinterpret_cast<u32x4_t*>(&Xl[b][(lrow + 32 * i) * kQRow + lcol]) = R[i];
-#pragma unroll
-      for (int i = 0; i < LB; ++i)
-        *reinterpret_cast<u32x4_t*>(&Wl[b][(lrow + 32 * i) * kQRow + lcol]) = R[LA + i];
-#pragma unroll
-      for (int i = 0; i < FM; ++i) sx[i] = sxn[i];
-      sw = swn;
-    };
-    gload(0);
-    lstore(0);
-    __syncthreads();
-    const int fr = (lane & 15) * kQRow + (lane >> 4) * 16;
+    // a wave without rows or columns of the tile only loads and waits
+    const bool active = wm * 64 < cur.rows && cur.n0 + wn * 64 < a.Nout;
+    int st = 0;
     for (int kt = 0; kt < KT; ++kt) {
-      const int b = kt & 1;
-      if (kt + 1 < KT) gload(kt + 1);
-      Piece<EXACT> fx[FM];
-#pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        const uint8_t* p = &Xl[b][(wm * 64 + i * 16) * kQRow + fr];
-        fx[i].set(*reinterpret_cast<const u32x4_t*>(p),
-                  *reinterpret_cast<const u32x4_t*>(p + 64), sx[i]);
+      if (kt + 1 < KT) wait_vmcnt<kMidLoadsX + kMidLoadsW>();
+      else wait_vmcnt<0>();
+      __builtin_amdgcn_s_barrier();
+      if (kt + 2 < KT) {
+        issue(kt + 2, st == 0 ? 2 : st - 1);
+        if ((kt & 15) == 0 && kt + 16 < KT) issue_scales((kt >> 4) + 1);
       }
+      if (active) {
+        const uint8_t* const xs = lds + st * kMidStage + wm * 64 * kBlk + fr;
+        const uint8_t* const ws = lds + st * kMidStage + kMidTileX + wn * 64 * kBlk + fr;
+        const uint32_t flip = 64u;  // chunk (lane / 16) + 4: the swizzle leaves bit 2 to the chunk
+        const uint8_t* const sc = s_sc[(kt >> 4) & 1] + (kt & 15);
+        const int sw = sc[(kMidTM + (wn >> 1)) * 16];
+        Piece<EXACT> px[FM];
 #pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const uint8_t* p = &Wl[b][(wn * WN + j * 16) * kQRow + fr];
-        Piece<EXACT> fw;
-        fw.set(*reinterpret_cast<const u32x4_t*>(p), *reinterpret_cast<const u32x4_t*>(p + 64),
-               sw);
+        for (int i = 0; i < FM; ++i) {
+          const uint32_t o = i * 16 * kBlk;
+          const uint8_t* const p = lds + ((uint32_t(xs - lds) + o) ^ flip);
+          px[i].set(*reinterpret_cast<const u32x4_t*>(xs + o), *reinterpret_cast<const u32x4_t*>(p),
+                    sc[(wm * 64 + i * 16 + (lane & 15)) * 16]);
+        }
 #pragma unroll
-        for (int i = 0; i < FM; ++i) acc[j][i] = mfma_q8(fw, fx[i], acc[j][i]);
+        for (int j = 0; j < FN; ++j) {
+          const uint32_t o = j * 16 * kBlk;
+          const uint8_t* const p = lds + ((uint32_t(ws - lds) + o) ^ flip);
+          Piece<EXACT> pw;
+          pw.set(*reinterpret_cast<const u32x4_t*>(ws + o), *reinterpret_cast<const u32x4_t*>(p),
+                 sw);
+#pragma unroll
+          for (int i = 0; i < FM; ++i) acc[j][i] = mfma_q8(pw, px[i], acc[j][i]);
+        }
       }
-      if (kt + 1 < KT) lstore(b ^ 1);
-      __syncthreads();
+      st = st == 2 ? 0 : st + 1;
     }
 
-    // the lane holds columns c .. c + 3 (c = 16 j + 4 (lane / 16)) of row
-    // (lane & 15) of each 16 x 16 tile
-    const int c0 = n0 + wn * WN + 4 * (lane >> 4);
+    int drow[FM];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) drow[i] = s_dst[wm * 64 + i * 16 + (lane & 15)];
+    __syncthreads();
+    if (has_next) {
+      start(nxt, nsrc, ndst);
+      begin();
+    }
+    const int c0 = cur.n0 + wn * 64 + 4 * (lane >> 4);
     if constexpr (KIND == kUp) {
-      const int No = kGated ? a.Nout / 2 : a.Nout;
-      // activation in place, then each row's largest magnitude over the block:
-      // the lane's, the four lanes of a row, the two waves of a row
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
         float top = 0.0f;
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          f32x4_t& v = acc[j][i];
-          const int c = c0 + 16 * j;
-          if constexpr (kGated) {
-            v[0] = c < a.Nout ? silu_f(v[0]) * v[1] : 0.0f;
-            v[1] = c + 2 < a.Nout ? silu_f(v[2]) * v[3] : 0.0f;
-            top = fmaxf(top, fmaxf(q8_mag(v[0]), q8_mag(v[1])));
-          } else {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              v[u] = c + u < No ? act_fn<ACT>(v[u]) : 0.0f;
-              top = fmaxf(top, q8_mag(v[u]));
-            }
-          }
-        }
+        for (int j = 0; j < FN; ++j) top = fmaxf(top, hidden4<ACT>(acc[j][i], c0 + 16 * j, a.Nout));
         top = fmaxf(top, __shfl_xor(top, 16, kWave));
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
         if (lane < 16) s_top[wn][wm * 64 + i * 16 + lane] = top;
       }
       __syncthreads();
-      const int blk = (kGated ? n0 / 2 : n0) / kBlk;
+      const int blk = (kGated ? cur.n0 / 2 : cur.n0) / kBlk + (kGated ? 0 : wn >> 1);
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
+        if (drow[i] < 0 || blk * kBlk >= a.qpitch) continue;
         const int row = wm * 64 + i * 16 + (lane & 15);
-        const int byte = q8_scale_byte(fmaxf(s_top[0][row], s_top[1][row]));
+        float top = fmaxf(s_top[wn & (kGated ? 0 : 2)][row], s_top[(wn & (kGated ? 0 : 2)) + 1][row]);
+        if (kGated) top = fmaxf(top, fmaxf(s_top[2][row], s_top[3][row]));
+        const int byte = q8_scale_byte(top);
         const float inv = q8_inv(byte);
-        const int64_t drow = s_dst[row];
-        if (drow < 0) continue;
-        if (wn == 0 && lane < 16) a.s[drow * a.qspitch + blk] = static_cast<uint8_t>(byte);
+        if ((wn & (kGated ? 3 : 1)) == 0 && lane < 16)
+          a.s[int64_t(drow[i]) * a.qspitch + blk] = static_cast<uint8_t>(byte);
+        uint8_t* const qrow = a.q + int64_t(drow[i]) * a.qpitch;
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          const f32x4_t v = acc[j][i];
-          const int c = c0 + 16 * j;
-          uint8_t* const p = a.q + drow * a.qpitch + (kGated ? c / 2 : c);
-          if constexpr (kGated)
-            *reinterpret_cast<uint16_t*>(p) =
-                static_cast<uint16_t>(q8_pack4(v[0] * inv, v[1] * inv, 0.0f, 0.0f));
-          else
-            *reinterpret_cast<uint32_t*>(p) =
-                q8_pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-        }
+        for (int j = 0; j < FN; ++j) store_hidden4<ACT>(qrow, c0 + 16 * j, acc[j][i], inv);
       }
     } else {
-      T* const og = static_cast<T*>(routed ? a.dst : a.dst_sh);
+      T* const og = static_cast<T*>(KIND == kDense || cur.e < a.E ? a.dst : a.dst_sh);
       const bool vec = (reinterpret_cast<uintptr_t>(og) & 15u) == 0 && a.ldo % 4 == 0;
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
-        const int64_t drow = s_dst[wm * 64 + i * 16 + (lane & 15)];
-        if (drow < 0) continue;
+        if (drow[i] < 0) continue;
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          const int c = c0 + 16 * j;
-          f32x4_t v = acc[j][i];
-          if (KIND == kDense && a.bias != nullptr) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-              if (c + u < a.Nout) v[u] += a.bias[c + u];
-          }
-          store4(og + drow * a.ldo + c, v, a.Nout - c, vec && c + 4 <= a.Nout);
-        }
+        for (int j = 0; j < FN; ++j)
+          store_out4(a, og + int64_t(drow[i]) * a.ldo, c0 + 16 * j, acc[j][i], vec);
       }
     }
-    __syncthreads();
+    if (!has_next) break;
+    L = Ln;
+    cur = nxt;
   }
 }
 
-constexpr int kQBlocksPerCu = 1;
+// ---------------------------------------------------------------------------
+// 256 x 256 tiles for many rows, 8-bit products only: 64 KB of a k-tile per 16.8
+// MFLOP instead of 48 KB per 8.4 (the tile above), so that neither what a CU can
+// load nor its LDS bounds the matrix instructions.
+//
+// The schedule is the 256 x 256 bf16 kernel's (ffn.hip), whose k-tile has the
+// same bytes: eight waves of 128 rows x 64 columns (2 x 4), two LDS buffers of a
+// k-tile, each in four 16 KB regions, rows X0 X1 and columns W0 W1; a k-tile is
+// four phases, X0 W0, X0 W1, X1 W1, X1 W0, each a memory slot (LDS reads, two
+// loads, one wait) and a matrix slot (8 instructions of 16 x 16 x 128); waves 4-7
+// run one slot behind waves 0-3.  A region is refilled one phase after its last
+// read and has seven phases to land.  The load stream goes on into the next tile.
+//
+// Scales: 16 k-tiles of a tile's rows and two weight blocks (258 x 16 bytes) come
+// in one piece, three buffers in turn (the next piece, or the next tile's first,
+// is on its way while one is read).  The extra load only makes the counted waits
+// a little longer.
+//
+// The rows of a tile, 256, 192 or 128, come from the lists kernel's table (dense:
+// from the host) as for the bf16 kernel.
+// ---------------------------------------------------------------------------
+constexpr int kTallTM = 256;
+constexpr int kTallTN = 256;
+constexpr int kTallWaves = 8;
+constexpr int kTallThreads = kTallWaves * kWave;
+constexpr int kTallHalf = 128 * kBlk;    // bytes of a region
+constexpr int kTallBuf = 4 * kTallHalf;  // X0 X1 W0 W1
+constexpr int kTallMinKT = 4;            // k-tiles
+constexpr int kTallScales = (kTallTM + 2) * 16;
+
+__device__ __forceinline__ void tall_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// One wait for both: at most N loads of this wave in flight (N < 16), every LDS
+// read returned.
+template <int N>
+__device__ __forceinline__ void tall_wait() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(N) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// c += w x with the accumulator in place.  The builtin leaves the compiler free to
+// put the sum elsewhere and to move the instruction past branches, barriers and
+// waits; with 128 accumulator registers of 256 that ended in spills between the
+// loads of the ring.  The operands' LDS reads are waited for by the caller
+// (tall_wait), two wait states follow any vector instruction that wrote one, each
+// accumulator is used once between two barriers, and the epilogue's first read is
+// held off (below): the distances that the hardware leaves to the program.
+__device__ __forceinline__ void mfma_q8_tied(f32x4_t& c, const i32x8_t& w, const i32x8_t& x,
+                                             int sw, int sx) {
+  asm volatile(
+      "s_nop 1\n\t"
+      "v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]"
+      : "+v"(c)
+      : "v"(w), "v"(x), "v"(sw), "v"(sx));
+}
+
+template <int KIND, int ACT, typename T>
+__global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
+  constexpr bool kGated = ACT == kActSwiglu;
+  constexpr bool kListed = KIND == kUp;  // token rows come through the list
+  constexpr bool kTable = KIND != kDense;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kTallBuf];
+  __shared__ __attribute__((aligned(16))) uint8_t s_sc[3 * kTallScales];
+  __shared__ int s_list[2][kTallTM];
+  __shared__ int s_toff[128];
+  __shared__ float s_top[KIND == kUp ? 2 : 1][4][kTallTM];
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wv >> 2, wn = wv & 3;  // wm is also the ping-pong group
+  const int TM = kTable ? *a.tm : a.dense_tm;
+  const int nt = (a.Nout + kTallTN - 1) / kTallTN;
+  const int total = kTable ? a.tile_off[a.G] : (a.M + TM - 1) / TM * nt;
+  const int per = (total + kXcds - 1) / kXcds;
+  const int lo = (blockIdx.x % kXcds) * per;
+  const int hi = min(total, lo + per);
+  const int stride = gridDim.x / kXcds;
+  if constexpr (kTable) {
+    if (tid < 128) s_toff[tid] = tid < a.G ? a.tile_off[tid] : 0x7fffffff;
+    __syncthreads();
+  }
+  const int KT = a.pitch / kBlk;
+  const int nbw = (a.Nout + kBlk - 1) / kBlk;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(lds) + wv * 1024);
+  const uint32_t sl0 = __builtin_amdgcn_readfirstlane(lds_addr(&s_list[0][0]) + (wv & 3) * 256);
+  const uint32_t sc0 = __builtin_amdgcn_readfirstlane(lds_addr(&s_sc[0]) + wv * 1024);
+
+  // the lane number, opaque to the compiler: what is derived from it at a tile's
+  // ends is computed there and not kept in registers across the k-loop
+  auto fresh_lane = [&]() __attribute__((always_inline)) {
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    return l;
+  };
+  struct TTile {
+    int e, r0, rows, n0;
+  };
+  auto tile = [&](int L) __attribute__((always_inline)) {
+    TTile t;
+    int e_base = 0, o0 = 0, cnt = a.M;
+    t.e = 0;
+    if constexpr (kTable) {
+      const int toff0 = s_toff[fresh_lane()], toff1 = s_toff[64 + fresh_lane()];
+      t.e = __builtin_amdgcn_readfirstlane(tile_group(L, toff0, toff1, e_base));
+      o0 = a.off[t.e];
+      cnt = a.off[t.e + 1] - o0;
+    }
+    const int mt = (cnt + TM - 1) / TM;
+    const int local = __builtin_amdgcn_readfirstlane(L - e_base);
+    const int m = local % mt;
+    t.r0 = __builtin_amdgcn_readfirstlane(o0 + static_cast<int>(int64_t(m) * cnt / mt));
+    t.rows = __builtin_amdgcn_readfirstlane(o0 + static_cast<int>(int64_t(m + 1) * cnt / mt) - t.r0);
+    t.n0 = __builtin_amdgcn_readfirstlane((local / mt) * kTallTN);
+    return t;
+  };
+
+  // the load stream's tile: byte offsets of this lane's rows, and of its scales'
+  uint32_t va[4], vw[4];
+  const uint8_t* wbase = a.W;
+  auto source = [&](const TTile& t, int lb, int r) __attribute__((always_inline)) {
+    const int rr = r < t.rows ? r : 0;
+    if (KIND == kDense) return t.r0 + rr;
+    if (KIND == kDown) return t.r0 + rr;
+    if (t.e >= a.E) return t.r0 + rr - a.off[t.e];
+    return s_list[lb][rr] / a.k;
+  };
+  auto aim = [&](const TTile& t, int lb) __attribute__((always_inline)) {
+    const int lane = fresh_lane();
+    const int chunk = (lane & 7) ^ (4 * (wv & 1) + (lane >> 4));
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int r = 128 * (q >> 1) + 8 * (wv + kTallWaves * (q & 1)) + (lane >> 3);
+      va[q] = static_cast<uint32_t>(source(t, lb, r)) * static_cast<uint32_t>(a.pitch) + chunk * 16;
+      const int n = min(r, a.Nout - 1 - t.n0);
+      vw[q] = static_cast<uint32_t>(n) * static_cast<uint32_t>(a.pitch) + chunk * 16;
+    }
+    const bool routed = !kTable || t.e < a.E;
+    wbase = (routed ? a.W : a.Wsh) + (int64_t(routed ? t.e : t.e - a.E) * a.Nout + t.n0) * a.pitch;
+  };
+  // piece c of a tile's scales into buffer b: waves 0-3 the rows', two lanes of
+  // wave 4 the weight blocks'
+  auto issue_scales = [&](const TTile& t, int lb, int c, int b) __attribute__((always_inline)) {
+    const int lane = fresh_lane();
+    const uint32_t to = __builtin_amdgcn_readfirstlane(sc0 + b * kTallScales);
+    if (wv < 4) {
+      dma16(reinterpret_cast<const uint16_t*>(
+                a.Xs + int64_t(source(t, lb, 64 * wv + lane)) * a.spitch + c * 16),
+            to);
+    } else if (wv == 4 && lane < 2) {
+      const bool routed = !kTable || t.e < a.E;
+      dma16(reinterpret_cast<const uint16_t*>(
+                (routed ? a.Ws : a.Wssh) +
+                (int64_t(routed ? t.e : t.e - a.E) * nbw + min(t.n0 / kBlk + lane, nbw - 1)) *
+                    a.spitch + c * 16),
+            __builtin_amdgcn_readfirstlane(to));
+    }
+  };
+  // row table of a tile into s_list[lb]: the list entries, fetched one tile ahead
+  // (up), or the output rows of the current tile (down)
+  auto fetch_list = [&](const TTile& t, int lb) __attribute__((always_inline)) {
+    const int lane = fresh_lane();
+    if (wv < 4 && t.e < a.E)
+      dma4((kListed ? a.list : a.row_dst) + t.r0 + min(64 * wv + lane, t.rows - 1),
+           sl0 + lb * (kTallTM * 4));
+  };
+  auto issue_x = [&](int kt, int b, int h, int nr) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (h == 0 || 128 + 64 * u < nr)
+        dma16_s(a.X + kt * kBlk, va[2 * h + u], lds0 + b * kTallBuf + h * kTallHalf + u * 8192);
+  };
+  auto issue_w = [&](int kt, int b, int h) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      dma16_s(wbase + kt * kBlk, vw[2 * h + u],
+              lds0 + b * kTallBuf + (2 + h) * kTallHalf + u * 8192);
+  };
+
+  const uint32_t fr = (lane & 15) * kBlk + (((lane >> 4) ^ ((lane >> 1) & 7)) * 16);
+  const uint8_t* const xl = lds + wm * 2048;
+  const uint8_t* const wl = lds + 2 * kTallHalf + wn * 4096;
+  const uint32_t sl = (lane & 15) * 16 + wm * 256;
+
+  i32x8_t fx[4], fa[2], fb[2];
+  int sx[4], sw0, sw1;
+  auto read_x = [&](int b, int h, int n) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i >= n) continue;
+      const uint8_t* const p = xl + b * kTallBuf + h * kTallHalf + i * 4096;
+      fx[i] = join(*reinterpret_cast<const u32x4_t*>(p + fr),
+                   *reinterpret_cast<const u32x4_t*>(p + (fr ^ 64)));
+    }
+  };
+  auto read_w = [&](i32x8_t (&f)[2], int b, int h) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint8_t* const p = wl + b * kTallBuf + h * kTallHalf + j * 2048;
+      f[j] = join(*reinterpret_cast<const u32x4_t*>(p + fr),
+                  *reinterpret_cast<const u32x4_t*>(p + (fr ^ 64)));
+    }
+  };
+  // sb: the scale buffer's offset plus the k-tile's byte
+  auto read_sx = [&](int sb, int h, int n) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) sx[i] = s_sc[sb + sl + h * 2048 + i * 512];
+  };
+
+  int L = lo + static_cast<int>(blockIdx.x) / kXcds;
+  if (L >= hi) return;
+  TTile cur = tile(L);
+  int lb = 0, sb = 0;      // row table and first buffer of the tile
+  int sc = 0;              // scale buffer of the k-tile (0, 1, 2)
+  if (kListed) fetch_list(cur, 0);
+  tall_wait<0>();
+  tall_barrier();
+  aim(cur, 0);
+  issue_scales(cur, 0, 0, 0);
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    issue_w(p, p, 0);
+    issue_x(p, p, 0, kTallTM);
+    issue_w(p, p, 1);
+    issue_x(p, p, 1, kTallTM);
+  }
+  tall_wait<0>();
+  tall_barrier();
+  read_w(fa, 0, 0);
+  tall_wait<0>();
+  tall_barrier();
+  if (wm == 1) tall_barrier();
+
+  f32x4_t acc[4][8];  // [column tile][row tile]
+  for (;;) {
+    const int Ln = L + stride;
+    const bool has_next = Ln < hi;
+    TTile nxt = cur;
+    if (has_next) nxt = tile(Ln);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[j][i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    // one instantiation per tile height (NX = 0, 2 or 4 16-row tiles per wave in
+    // the second half), with or without columns past 128 (CA)
+    auto run = [&](auto nx_c, auto ca_c) __attribute__((always_inline)) {
+      constexpr int NX = decltype(nx_c)::value;
+      constexpr bool CA = decltype(ca_c)::value;
+      auto mfma_q = [&](int h, int c, const i32x8_t (&f)[2], int sw) __attribute__((always_inline)) {
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (h == 0 || i < NX)
+              mfma_q8_tied(acc[2 * c + j][4 * h + i], f[j], fx[i], sw, sx[i]);
+        __builtin_amdgcn_s_setprio(0);
+      };
+      auto ktile = [&](int t, int b, i32x8_t (&p)[2], i32x8_t (&q)[2], auto tail_c)
+          __attribute__((always_inline)) {
+        constexpr bool kTail = decltype(tail_c)::value;
+        const int lt = kTail ? t + 2 - KT : t + 2;
+        constexpr int nx = kTail || NX == 4 ? 256 : NX == 2 ? 192 : 128;
+        const int so = __builtin_amdgcn_readfirstlane(sc * kTallScales + (t & 15));
+        auto settle = [&]() __attribute__((always_inline)) {
+          tall_wait<kTail ? 8 : 8 + NX>();
+          tall_barrier();
+        };
+        // phase 0: X0 x W0
+        read_x(b, 0, 4);
+        read_sx(so, 0, 4);
+        sw0 = s_sc[so + kTallTM * 16];
+        sw1 = s_sc[so + kTallTM * 16 + 16];
+        issue_w(lt, b, 0);
+        settle();
+        mfma_q(0, 0, p, sw0);
+        tall_barrier();
+        // phase 1: X0 x W1
+        if (CA) read_w(q, b, 1);
+        issue_x(lt, b, 0, nx);
+        settle();
+        if (CA) mfma_q(0, 1, q, sw1);
+        tall_barrier();
+        // phase 2: X1 x W1
+        if (NX > 0) {
+          read_x(b, 1, NX);
+          read_sx(so, 1, NX);
+        }
+        issue_w(lt, b, 1);
+        settle();
+        if (CA && NX > 0) mfma_q(1, 1, q, sw1);
+        tall_barrier();
+        // phase 3: X1 x W0, and the next k-tile's W0
+        read_w(q, b ^ 1, 0);
+        issue_x(lt, b, 1, nx);
+        settle();
+        if (NX > 0) mfma_q(1, 0, p, sw0);
+        tall_barrier();
+      };
+      // No branches inside a k-tile: tables and scales are asked for between them,
+      // and the last tile's last two k-tiles load as the others' do (its own first
+      // ones, again).
+      auto advance = [&](int done) __attribute__((always_inline)) {
+        sc = (done & 15) != 15 ? sc : sc == 2 ? 0 : sc + 1;
+      };
+      int t = 0;
+      for (; t < KT - 3; t += 2) {
+        if ((t & 15) == 0) {
+          // the row table of this tile (down) or the next one (up), in the buffer
+          // that the previous tile's epilogue does not read
+          if (t == 0 && KIND == kDown) fetch_list(cur, lb);
+          if (t == 0 && kListed && has_next) fetch_list(nxt, lb ^ 1);
+          if (t + 16 < KT) issue_scales(cur, lb, (t >> 4) + 1, sc == 2 ? 0 : sc + 1);
+        }
+        ktile(t, sb, fa, fb, std::false_type{});
+        ktile(t + 1, sb ^ 1, fb, fa, std::false_type{});
+        advance(t + 1);
+      }
+      if (t == KT - 3) {
+        // odd count: one more, and its roles exchanged back
+        ktile(t, sb, fa, fb, std::false_type{});
+#pragma unroll
+        for (int j = 0; j < 2; ++j) fa[j] = fb[j];
+        sb ^= 1;
+        advance(t);
+      }
+      if (has_next) {
+        aim(nxt, lb ^ 1);
+        // into the next buffer, or past the one that this tile's last k-tile reads
+        issue_scales(nxt, lb ^ 1, 0, (sc + (((KT - 2) & 15) == 15 ? 2 : 1)) % 3);
+      }
+      ktile(KT - 2, sb, fa, fb, std::true_type{});
+      advance(KT - 2);
+      ktile(KT - 1, sb ^ 1, fb, fa, std::true_type{});
+      // what reads the accumulators comes after this
+      asm volatile("s_nop 15\n\ts_nop 15");
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(acc[j][i]));
+    };
+    if (cur.n0 + 128 < a.Nout) {
+      if (cur.rows > 192) run(std::integral_constant<int, 4>{}, std::true_type{});
+      else if (cur.rows > 128) run(std::integral_constant<int, 2>{}, std::true_type{});
+      else run(std::integral_constant<int, 0>{}, std::true_type{});
+    } else {
+      if (cur.rows > 192) run(std::integral_constant<int, 4>{}, std::false_type{});
+      else if (cur.rows > 128) run(std::integral_constant<int, 2>{}, std::false_type{});
+      else run(std::integral_constant<int, 0>{}, std::false_type{});
+    }
+
+    // epilogue: tile 2 c + j of columns starts at n0 + 128 c + 32 wn + 16 j, tile i
+    // of rows at 128 (i / 4) + 16 (2 (i % 4) + wm).  Lanes l and l ^ 16 exchange
+    // runs of a wave's two adjacent column tiles, so that a store writes 8
+    // consecutive columns (hidden: 8 bytes, gated 4).
+    const int lane = fresh_lane();
+    const int g = lane >> 4, odd = g & 1;
+    if constexpr (KIND == kUp) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int row = 128 * (i >> 2) + 16 * (2 * (i & 3) + wm) + (lane & 15);
+        float top[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int c0 = cur.n0 + 128 * c + 32 * wn + 4 * g;
+          top[c] = fmaxf(hidden4<ACT>(acc[2 * c][i], c0, a.Nout),
+                         hidden4<ACT>(acc[2 * c + 1][i], c0 + 16, a.Nout));
+        }
+        if (kGated) top[0] = fmaxf(top[0], top[1]);
+#pragma unroll
+        for (int c = 0; c < (kGated ? 1 : 2); ++c) {
+          top[c] = fmaxf(top[c], __shfl_xor(top[c], 16, kWave));
+          top[c] = fmaxf(top[c], __shfl_xor(top[c], 32, kWave));
+          if (lane < 16) s_top[c][wn][row] = top[c];
+        }
+      }
+      tall_wait<15>();
+      tall_barrier();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int row = 128 * (i >> 2) + 16 * (2 * (i & 3) + wm) + (lane & 15);
+        if (row >= cur.rows) continue;
+        const int64_t drow = cur.r0 + row;
+        uint8_t* const qrow = a.q + drow * a.qpitch;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int blk = kGated ? cur.n0 / 2 / kBlk : cur.n0 / kBlk + c;
+          if (blk * kBlk >= a.qpitch) continue;
+          const int tc = kGated ? 0 : c;
+          const int byte = q8_scale_byte(fmaxf(fmaxf(s_top[tc][0][row], s_top[tc][1][row]),
+                                               fmaxf(s_top[tc][2][row], s_top[tc][3][row])));
+          const float inv = q8_inv(byte);
+          if (wn == 0 && lane < 16 && (!kGated || c == 0))
+            a.s[drow * a.qspitch + blk] = static_cast<uint8_t>(byte);
+          const f32x4_t &v0 = acc[2 * c][i], &v1 = acc[2 * c + 1][i];
+          const int cw = cur.n0 + 128 * c + 32 * wn;
+          if constexpr (kGated) {
+            const uint32_t p0 = q8_pack4(v0[0] * inv, v0[1] * inv, 0.0f, 0.0f) & 0xffffu;
+            const uint32_t p1 = q8_pack4(v1[0] * inv, v1[1] * inv, 0.0f, 0.0f) & 0xffffu;
+            const uint32_t r = __shfl_xor(odd ? p0 : p1, 16, kWave);
+            *reinterpret_cast<uint32_t*>(qrow + cw / 2 + 8 * odd + 2 * (g - odd)) =
+                odd ? (r | (p1 << 16)) : (p0 | (r << 16));
+          } else {
+            const uint32_t p0 = q8_pack4(v0[0] * inv, v0[1] * inv, v0[2] * inv, v0[3] * inv);
+            const uint32_t p1 = q8_pack4(v1[0] * inv, v1[1] * inv, v1[2] * inv, v1[3] * inv);
+            const uint32_t r = __shfl_xor(odd ? p0 : p1, 16, kWave);
+            *reinterpret_cast<u32x2_t*>(qrow + cw + 16 * odd + 4 * (g - odd)) =
+                odd ? u32x2_t{r, p1} : u32x2_t{p0, r};
+          }
+        }
+      }
+    } else {
+      T* const og = static_cast<T*>(!kTable || cur.e < a.E ? a.dst : a.dst_sh);
+      const bool vec = (reinterpret_cast<uintptr_t>(og) & 15u) == 0 && a.ldo % 8 == 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int row = 128 * (i >> 2) + 16 * (2 * (i & 3) + wm) + (lane & 15);
+        if (row >= cur.rows) continue;
+        int64_t drow = cur.r0 + row;
+        if (KIND == kDown) drow = cur.e < a.E ? s_list[lb][row] : drow - a.off[a.E];
+        T* const orow = og + drow * a.ldo;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int cw = cur.n0 + 128 * c + 32 * wn;  // first column of the pair
+          if (cw >= a.Nout) continue;
+          f32x4_t v[2] = {acc[2 * c][i], acc[2 * c + 1][i]};
+          if (sizeof(T) == 2 && vec && cw + 32 <= a.Nout) {
+            if (KIND == kDense && a.bias != nullptr) {
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v[j][u] += a.bias[cw + 16 * j + 4 * g + u];
+            }
+            u32x2_t pk[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+              pk[j] = u32x2_t{pack2_bf16(v[j][0], v[j][1]), pack2_bf16(v[j][2], v[j][3])};
+            const u32x2_t keep = odd ? pk[1] : pk[0];
+            const u32x2_t send = odd ? pk[0] : pk[1];
+            const uint32_t q0 = __shfl_xor(send[0], 16, kWave);
+            const uint32_t q1 = __shfl_xor(send[1], 16, kWave);
+            *reinterpret_cast<u32x4_t*>(orow + cw + 16 * odd + 4 * (g - odd)) =
+                odd ? u32x4_t{q0, q1, keep[0], keep[1]} : u32x4_t{keep[0], keep[1], q0, q1};
+          } else {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+              store_out4(a, orow, cw + 16 * j + 4 * g, v[j], vec);
+          }
+        }
+      }
+    }
+    if (!has_next) break;
+    // the next tile's first piece of scales
+    sc = sc == 2 ? 0 : sc + 1;
+    L = Ln;
+    cur = nxt;
+    lb ^= 1;
+  }
+  if (wm == 0) tall_barrier();
+  tall_wait<0>();  // the last loads have landed before the LDS is given up
+}
 
 template <int KIND, int ACT, typename T, bool EXACT>
 hipError_t launch(const QArgs& a, hipStream_t st) {
-  launch_kernel(&qgemm_kernel<KIND, ACT, T, EXACT>, dim3(device_cus() * kQBlocksPerCu), dim3(kQThreads),
-                0, st, a);
+  launch_kernel(&qgemm_mid_kernel<KIND, ACT, T, EXACT>, dim3(device_cus()), dim3(kMidThreads), 0,
+                st, a);
   return hipGetLastError();
 }
 
-template <bool EXACT>
-hipError_t launch_act(int act, const QArgs& a, hipStream_t st) {
-  if (act == MOECA_ACT_SWIGLU) return launch<kUp, kActSwiglu, float, EXACT>(a, st);
-  if (act == MOECA_ACT_GELU_ERF) return launch<kUp, kActGeluErf, float, EXACT>(a, st);
-  return launch<kUp, kActGeluTanh, float, EXACT>(a, st);
+template <int KIND, int ACT, typename T>
+hipError_t launch_tall(const QArgs& a, hipStream_t st) {
+  launch_kernel(&qgemm_tall_kernel<KIND, ACT, T>, dim3(device_cus()), dim3(kTallThreads), 0, st,
+                a);
+  return hipGetLastError();
+}
+
+template <int ACT>
+hipError_t launch_up(const QArgs& a, bool exact, bool tall, hipStream_t st) {
+  if (tall) return launch_tall<kUp, ACT, float>(a, st);
+  if (exact) return launch<kUp, ACT, float, true>(a, st);
+  return launch<kUp, ACT, float, false>(a, st);
+}
+
+// Whether the 256 x 256 tiles can take a product: rows addressed by 32-bit byte
+// offsets, K long enough for the load stream's lookahead.
+bool tall_capable(int64_t rows, int K) {
+  return q8_pitch(K) / kBlk >= kTallMinKT && rows * q8_pitch(K) < (int64_t(1) << 32);
 }
 
 // Whether the up projection takes the exact products (above).
@@ -381,17 +955,19 @@ Q8 q8_view(void* base, int64_t rows, int64_t K) {
 
 FfnPlan q8_plan(const Shape& s, StepKind kind, int64_t rows) {
   (void)kind;
-  (void)rows;
   FfnPlan p;
-  p.tm = p.tm_up = kQTM;
-  p.tn_up = s.swiglu ? 256 : 128;
-  p.tn_down = 128;
+  p.tm = p.tm_up = kMidTM;
+  p.tn_up = p.tn_down = kMidTN;
+  const bool many = rows / s.E >= 144;
+  p.tall_up = many && !exact_up(s) && tall_capable(s.tokens(), s.d);
+  p.tall_down = many && s.bf16 && tall_capable(s.mid_rows(), s.d_ff);
+  if (p.tall_up) p.tm_up = kTallTM;
+  if (p.tall_down) p.tm = kTallTM;
   return p;
 }
 
 hipError_t launch_q8_up(const Shape& s, int act, const FfnPlan& plan, const QuantWeights& w,
                         const Buffers& b, hipStream_t st) {
-  (void)plan;
   QArgs a{};
   const Q8 x = q8_view(b.x8, s.tokens(), s.d), mid = q8_view(b.mid, s.mid_rows(), s.d_ff);
   a.X = x.q;
@@ -414,13 +990,15 @@ hipError_t launch_q8_up(const Shape& s, int act, const FfnPlan& plan, const Quan
   a.s = mid.s;
   a.qpitch = static_cast<int>(q8_pitch(s.d_ff));
   a.qspitch = static_cast<int>(q8_spitch(s.d_ff));
-  if (exact_up(s)) return launch_act<true>(act, a, st);
-  return launch_act<false>(act, a, st);
+  a.tm = b.tiles + 2 * (s.groups() + 1);
+  const bool exact = exact_up(s);
+  if (act == MOECA_ACT_SWIGLU) return launch_up<kActSwiglu>(a, exact, plan.tall_up, st);
+  if (act == MOECA_ACT_GELU_ERF) return launch_up<kActGeluErf>(a, exact, plan.tall_up, st);
+  return launch_up<kActGeluTanh>(a, exact, plan.tall_up, st);
 }
 
 hipError_t launch_q8_down(const Shape& s, const FfnPlan& plan, const QuantWeights& w,
                           const Buffers& b, hipStream_t st) {
-  (void)plan;
   QArgs a{};
   const Q8 mid = q8_view(b.mid, s.mid_rows(), s.d_ff);
   a.X = mid.q;
@@ -442,6 +1020,8 @@ hipError_t launch_q8_down(const Shape& s, const FfnPlan& plan, const QuantWeight
   a.ldo = s.d;
   a.dst = s.cache8 ? b.fresh : b.h_c;
   a.dst_sh = b.h_sh;
+  a.tm = b.tiles + 2 * (s.groups() + 1) + 1;
+  if (plan.tall_down) return launch_tall<kDown, kActNone, uint16_t>(a, st);
   if (s.bf16) return launch<kDown, kActNone, uint16_t, false>(a, st);
   return launch<kDown, kActNone, float, true>(a, st);
 }
@@ -461,6 +1041,10 @@ hipError_t launch_q8_linear(const Q8& x, int64_t M, int K, const void* W, const 
   a.ldo = ldo;
   a.bias = bias;
   a.dst = out;
+  if (bf16 && M >= 256 && tall_capable(M, K)) {
+    a.dense_tm = tall_rows_one(M, (N + kTallTN - 1) / kTallTN, device_cus());
+    return launch_tall<kDense, kActNone, uint16_t>(a, st);
+  }
   if (bf16) return launch<kDense, kActNone, uint16_t, false>(a, st);
   return launch<kDense, kActNone, float, true>(a, st);
 }

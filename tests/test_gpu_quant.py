@@ -165,7 +165,10 @@ def _linear_bound(x, w, y, dtype, K):
     (7, 1000, 257, 5, True), (15, 128, 64, 0, True), (16, 2304, 576, 8, False),
     (17, 640, 1000, 0, True), (33, 4608, 1152, 0, True), (64, 1152, 1728, 0, False),
     (65, 320, 70, 2, True), (129, 1000, 1730, 0, True), (200, 2100, 300, 0, False),
-    (513, 1152, 1152, 0, True), (1000, 192, 2305, 4, False), (2049, 1280, 640, 0, True)])
+    (513, 1152, 1152, 0, True), (1000, 192, 2305, 4, False), (2049, 1280, 640, 0, True),
+    # 17, 33, 31 and 4 blocks of K: pieces of 16 scales that end in the last blocks
+    (300, 2100, 700, 0, True), (777, 4224, 130, 0, False), (700, 3968, 520, 0, True),
+    (900, 512, 1100, 8, True), (5000, 640, 2500, 0, True)])
 def test_linear(M, K, N, extra, bias, dtype):
     import torch
     from paper_2606_15615_amd import quant
