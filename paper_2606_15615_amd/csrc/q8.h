@@ -24,17 +24,22 @@ __host__ __device__ constexpr int64_t q8_spitch(int64_t K) {
   return ((K + kBlk - 1) / kBlk + 15) / 16 * 16;
 }
 
-// |v| where v is finite, else 0: what a block's scale is chosen from.
-__device__ __forceinline__ float q8_mag(float v) {
-  const float a = __uint_as_float(__float_as_uint(v) & 0x7fffffffu);
-  return a < __uint_as_float(0x7f800000u) ? a : 0.0f;
+// Magnitudes are compared as bits (sign cleared, their order is the numeric one;
+// infinities and NaN come last, from kInfBits on): one instruction for the
+// largest of three, where a float maximum would first quieten its operands.
+constexpr uint32_t kInfBits = 0x7f800000u;
+__device__ __forceinline__ uint32_t q8_mag(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+// The same with 0 for what is not finite: what a block's scale is chosen from.
+__device__ __forceinline__ uint32_t q8_finite(float v) {
+  const uint32_t b = q8_mag(v);
+  return b < kInfBits ? b : 0u;
 }
 
-// The scale byte of a block whose largest finite magnitude is `top`.  In bits:
-// top = m 2^x with 1 <= m < 2 needs e = x - 8, or one more when m > 1.75, which
-// is when adding 0x1fffff to the mantissa carries into the exponent.
-__device__ __forceinline__ int q8_scale_byte(float top) {
-  const int b = static_cast<int>((__float_as_uint(top) + 0x1fffffu) >> 23) - 8;
+// The scale byte of a block whose largest finite magnitude has the bits `top`:
+// m 2^x with 1 <= m < 2 needs e = x - 8, or one more when m > 1.75, which is when
+// adding 0x1fffff to the mantissa carries into the exponent.
+__device__ __forceinline__ int q8_scale_byte(uint32_t top) {
+  const int b = static_cast<int>((top + 0x1fffffu) >> 23) - 8;
   return b > 0 ? b : 0;
 }
 // 2^-e and 2^e of a scale byte (0..247 as q8_scale_byte gives them; 2^-127 is
@@ -46,15 +51,11 @@ __device__ __forceinline__ float q8_two(int byte) {
   return __uint_as_float(byte > 0 ? static_cast<uint32_t>(byte) << 23 : 0x00400000u);
 }
 
-// Four values, already divided by their scale, to e4m3 (nearest, ties to even);
-// what is not finite becomes NaN.
+// Four values, already divided by their scale (at most 448, or not finite), to
+// e4m3: nearest, ties to even; the conversion makes NaN of NaN and infinities.
 __device__ __forceinline__ uint32_t q8_pack4(float a, float b, float c, float d) {
-  auto fin = [](float v) {
-    return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? __uint_as_float(0x7fc00000u) : v;
-  };
-  int p = __builtin_amdgcn_cvt_pk_fp8_f32(fin(a), fin(b), 0, false);
-  p = __builtin_amdgcn_cvt_pk_fp8_f32(fin(c), fin(d), p, true);
-  return static_cast<uint32_t>(p);
+  const int p = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, p, true));
 }
 
 typedef __attribute__((ext_vector_type(2))) float q8_f32x2;
@@ -68,11 +69,13 @@ __device__ __forceinline__ void q8_unpack4(uint32_t p, float* v) {
 }
 
 // Largest of a 16-lane row's values, in every lane of the row.
-__device__ __forceinline__ float row_max_f32(float v) {
-  v = fmaxf(v, dpp_f32<kDppRow[0]>(v));
-  v = fmaxf(v, dpp_f32<kDppRow[1]>(v));
-  v = fmaxf(v, dpp_f32<kDppRow[2]>(v));
-  return fmaxf(v, dpp_f32<kDppRow[3]>(v));
+__device__ __forceinline__ uint32_t row_max_u32(uint32_t v) {
+  auto step = [&](int o) { v = max(v, static_cast<uint32_t>(o)); };
+  step(dpp_i32<kDppRow[0]>(static_cast<int>(v)));
+  step(dpp_i32<kDppRow[1]>(static_cast<int>(v)));
+  step(dpp_i32<kDppRow[2]>(static_cast<int>(v)));
+  step(dpp_i32<kDppRow[3]>(static_cast<int>(v)));
+  return v;
 }
 
 // Eight elements from p (16-byte aligned when VEC), those at or past n as 0.
@@ -123,10 +126,15 @@ __device__ __forceinline__ void store8(T* p, int n, const float* v) {
 // Eight elements of a lane, 16 lanes to a block: the block's scale byte (in
 // every lane of the row) and the lane's eight bytes.
 __device__ __forceinline__ uint2 q8_quant8(const float* v, int& byte) {
-  float top = 0.0f;
+  uint32_t top = 0;
 #pragma unroll
-  for (int u = 0; u < 8; ++u) top = fmaxf(top, q8_mag(v[u]));
-  byte = q8_scale_byte(row_max_f32(top));
+  for (int u = 0; u < 8; ++u) top = max(top, q8_mag(v[u]));
+  if (__builtin_expect(__any(top >= kInfBits), 0)) {
+    top = 0;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) top = max(top, q8_finite(v[u]));
+  }
+  byte = q8_scale_byte(row_max_u32(top));
   const float inv = q8_inv(byte);
   return make_uint2(q8_pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
                     q8_pack4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));

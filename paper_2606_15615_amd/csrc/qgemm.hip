@@ -85,6 +85,8 @@ template <> struct Piece<false> {
     v = join(a, b);
     s = byte;
   }
+  // computed by here, whatever the compiler would rather
+  __device__ __forceinline__ void pin() {}
 };
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_q;
 template <> struct Piece<true> {
@@ -106,17 +108,11 @@ template <> struct Piece<true> {
       v[h] = __builtin_bit_cast(bf16x8_t, o);
     }
   }
-};
-
-__device__ __forceinline__ f32x4_t mfma_q8(const Piece<false>& w, const Piece<false>& x,
-                                           f32x4_t c) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.v, x.v, c, 0, 0, 0, w.s, 0, x.s);
-}
-__device__ __forceinline__ f32x4_t mfma_q8(const Piece<true>& w, const Piece<true>& x, f32x4_t c) {
+  __device__ __forceinline__ void pin() {
 #pragma unroll
-  for (int h = 0; h < 4; ++h) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.v[h], x.v[h], c, 0, 0, 0);
-  return c;
-}
+    for (int h = 0; h < 4; ++h) asm volatile("" : "+v"(v[h]));
+  }
+};
 
 typedef __attribute__((ext_vector_type(2))) float f32x2_q;
 // Two fp32 -> two bf16 (hardware round to nearest even), packed in 4 bytes.
@@ -151,22 +147,36 @@ __device__ __forceinline__ void store4(T* p, f32x4_t v, int n, bool whole) {
 
 // The activation of an accumulator tile in place (gated: the two hidden values
 // in v[0], v[1]), zeros in hidden columns past the width (their weight rows are
-// clamped), and the largest magnitude.
+// clamped; whole: there are none), and the largest magnitude's bits.
 template <int ACT>
-__device__ __forceinline__ float hidden4(f32x4_t& v, int c, int Nout) {
+__device__ __forceinline__ uint32_t hidden4(f32x4_t& v, int c, int Nout, bool whole) {
   if constexpr (ACT == kActSwiglu) {
-    v[0] = c < Nout ? silu_f(v[0]) * v[1] : 0.0f;
-    v[1] = c + 2 < Nout ? silu_f(v[2]) * v[3] : 0.0f;
-    return fmaxf(q8_mag(v[0]), q8_mag(v[1]));
+    v[0] = silu_f(v[0]) * v[1];
+    v[1] = silu_f(v[2]) * v[3];
+    if (!whole) {
+      if (c >= Nout) v[0] = 0.0f;
+      if (c + 2 >= Nout) v[1] = 0.0f;
+    }
+    return max(q8_mag(v[0]), q8_mag(v[1]));
   } else {
-    float top = 0.0f;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      v[u] = c + u < Nout ? act_fn<ACT>(v[u]) : 0.0f;
-      top = fmaxf(top, q8_mag(v[u]));
+      v[u] = act_fn<ACT>(v[u]);
+      if (!whole && c + u >= Nout) v[u] = 0.0f;
     }
-    return top;
+    return max(max(q8_mag(v[0]), q8_mag(v[1])), max(q8_mag(v[2]), q8_mag(v[3])));
   }
+}
+// The largest finite magnitude of a tile's hidden values.
+template <int ACT>
+__device__ __forceinline__ uint32_t hidden_finite4(const f32x4_t& v) {
+  const uint32_t t = max(q8_finite(v[0]), q8_finite(v[1]));
+  return ACT == kActSwiglu ? t : max(t, max(q8_finite(v[2]), q8_finite(v[3])));
+}
+// Largest over the four lanes of a row.
+__device__ __forceinline__ uint32_t quad_max(uint32_t t) {
+  t = max(t, static_cast<uint32_t>(__shfl_xor(static_cast<int>(t), 16, kWave)));
+  return max(t, static_cast<uint32_t>(__shfl_xor(static_cast<int>(t), 32, kWave)));
 }
 
 // Quantised hidden values of a tile into their row, from hidden column c (gated:
@@ -191,6 +201,18 @@ __device__ __forceinline__ void store_out4(const QArgs& a, T* row, int c, f32x4_
   store4(row + c, v, a.Nout - c, vec && c + 4 <= a.Nout);
 }
 
+// Tile `local` of a group of mt x nt tiles: bands of eight row tiles, in a band the
+// column tiles in turn, each with all of the band's rows.  The 32 CUs of an XCD,
+// on consecutive tiles, then share eight row and four column tiles in its L2
+// (without bands, and 64 row tiles, each CU had rows of its own).
+__device__ __forceinline__ void band_order(int local, int mt, int nt, int& m, int& n) {
+  const int band = local / (8 * nt);
+  const int in = local - band * 8 * nt;
+  const int h = min(8, mt - band * 8);
+  n = in / h;
+  m = band * 8 + in - n * h;
+}
+
 // Source and destination row of row r of a tile (`rows` rows from r0 on).
 template <int KIND>
 __device__ __forceinline__ void tile_row(const QArgs& a, int e, int r0, int rows, int r, int& src,
@@ -204,13 +226,50 @@ __device__ __forceinline__ void tile_row(const QArgs& a, int e, int r0, int rows
 }
 
 // ---------------------------------------------------------------------------
+// Two groups of four waves take turns: a group's memory slot (LDS reads, loads of
+// the ring, one wait) runs beside the other's matrix slot, a barrier after each,
+// so that on every SIMD one wave multiplies while the other reads.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ void slot_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// One wait for both: at most N loads of this wave in flight (N < 16), every LDS
+// read returned.
+template <int N>
+__device__ __forceinline__ void slot_wait() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(N) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// c += w x with the accumulator in place.  The builtin leaves the compiler free to
+// put the sum elsewhere and to move the instruction past branches, barriers and
+// waits; with 128 accumulator registers of 256 that ended in spills between the
+// loads of the ring.  The operands' LDS reads are waited for by the caller
+// (slot_wait), two wait states follow any vector instruction that wrote one, each
+// accumulator is used once between two barriers, and the epilogue's first read is
+// held off (below): the distances that the hardware leaves to the program.
+__device__ __forceinline__ void mfma_q8_tied(f32x4_t& c, const i32x8_t& w, const i32x8_t& x,
+                                             int sw, int sx) {
+  asm volatile(
+      "s_nop 1\n\t"
+      "v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]"
+      : "+v"(c)
+      : "v"(w), "v"(x), "v"(sw), "v"(sx));
+}
+
+// ---------------------------------------------------------------------------
 // 128 x 256 tiles: 8 waves (2 x 4) of 64 rows x 64 columns, 4 x 4 tiles of
 // 16 x 16 each (weights the A operand).  A k-tile is 128 bytes of every row, one
 // block; three of them (48 KB each) are in LDS or on their way, brought by direct
 // global -> LDS loads in the XOR-swizzled order of the bf16 kernels: position p
 // of row r holds 16-byte chunk p ^ ((r >> 1) & 7).  The scales come the same
 // way, 16 bytes (16 k-tiles) of each row at a time, into one of two buffers; a
-// k-tile's are read as bytes.  An up projection's block of 128 hidden columns
+// k-tile's are read as bytes.  The two groups are the tile's halves of rows; EXACT
+// converts its operands in the memory slot.  An up projection's block of 128 hidden columns
 // lies with two waves of a row (gated: four), which exchange their largest
 // magnitudes through LDS.  Persistent, one block per CU; the next tile's first
 // loads start before this tile's epilogue.
@@ -226,6 +285,14 @@ constexpr int kMidLoadsX = kMidTM / 8 / kMidWaves;     // 2 per wave and stage
 constexpr int kMidLoadsW = kMidTN / 8 / kMidWaves;     // 4
 constexpr int kMidScales = (kMidTM + 2) * 16;          // bytes of a scale buffer: rows, two blocks
 
+__device__ __forceinline__ void mfma_q8(const Piece<false>& w, const Piece<false>& x, f32x4_t& c) {
+  mfma_q8_tied(c, w.v, x.v, w.s, x.s);
+}
+__device__ __forceinline__ void mfma_q8(const Piece<true>& w, const Piece<true>& x, f32x4_t& c) {
+#pragma unroll
+  for (int h = 0; h < 4; ++h) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.v[h], x.v[h], c, 0, 0, 0);
+}
+
 template <int KIND, int ACT, typename T, bool EXACT>
 __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
   constexpr bool kGated = ACT == kActSwiglu;
@@ -233,7 +300,7 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[kMidStages * kMidStage];
   __shared__ __attribute__((aligned(16))) uint8_t s_sc[2][kMidScales];
   __shared__ int s_src[kMidTM], s_dst[kMidTM];
-  __shared__ float s_top[KIND == kUp ? 4 : 1][kMidTM];
+  __shared__ uint32_t s_top[KIND == kUp ? 4 : 1][kMidTM];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -269,12 +336,12 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
       cnt = a.off[t.e + 1] - o0;
     }
     const int mt = (cnt + kMidTM - 1) / kMidTM;
-    const int local = L - e_base;
-    const int m = local % mt;
+    int m, n;
+    band_order(L - e_base, mt, nt, m, n);
     t.e = __builtin_amdgcn_readfirstlane(t.e);
     t.r0 = __builtin_amdgcn_readfirstlane(o0 + m * kMidTM);
     t.rows = __builtin_amdgcn_readfirstlane(min(kMidTM, cnt - m * kMidTM));
-    t.n0 = __builtin_amdgcn_readfirstlane((local / mt) * kMidTN);
+    t.n0 = __builtin_amdgcn_readfirstlane(n * kMidTN);
     return t;
   };
 
@@ -326,6 +393,11 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
     issue(0, 0);
     if (KT > 1) issue(1, 1);
   };
+  auto first_landed = [&]() __attribute__((always_inline)) {
+    if (KT > 1) slot_wait<kMidLoadsX + kMidLoadsW>();
+    else slot_wait<0>();
+    slot_barrier();
+  };
 
   int L = lo + static_cast<int>(blockIdx.x) / kXcds;
   if (L >= hi) return;
@@ -354,41 +426,63 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
       for (int i = 0; i < FM; ++i) acc[j][i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     // a wave without rows or columns of the tile only loads and waits
     const bool active = wm * 64 < cur.rows && cur.n0 + wn * 64 < a.Nout;
+    first_landed();
+    if (wm == 1) slot_barrier();
     int st = 0;
     for (int kt = 0; kt < KT; ++kt) {
-      if (kt + 1 < KT) wait_vmcnt<kMidLoadsX + kMidLoadsW>();
-      else wait_vmcnt<0>();
-      __builtin_amdgcn_s_barrier();
-      if (kt + 2 < KT) {
-        issue(kt + 2, st == 0 ? 2 : st - 1);
-        if ((kt & 15) == 0 && kt + 16 < KT) issue_scales((kt >> 4) + 1);
-      }
+      // memory slot
+      Piece<EXACT> px[FM], pw[FN];
       if (active) {
-        const uint8_t* const xs = lds + st * kMidStage + wm * 64 * kBlk + fr;
-        const uint8_t* const ws = lds + st * kMidStage + kMidTileX + wn * 64 * kBlk + fr;
-        const uint32_t flip = 64u;  // chunk (lane / 16) + 4: the swizzle leaves bit 2 to the chunk
+        const uint32_t xo = st * kMidStage + wm * 64 * kBlk + fr;
+        const uint32_t wo = st * kMidStage + kMidTileX + wn * 64 * kBlk + fr;
         const uint8_t* const sc = s_sc[(kt >> 4) & 1] + (kt & 15);
         const int sw = sc[(kMidTM + (wn >> 1)) * 16];
-        Piece<EXACT> px[FM];
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-          const uint32_t o = i * 16 * kBlk;
-          const uint8_t* const p = lds + ((uint32_t(xs - lds) + o) ^ flip);
-          px[i].set(*reinterpret_cast<const u32x4_t*>(xs + o), *reinterpret_cast<const u32x4_t*>(p),
+          const uint32_t o = xo + i * 16 * kBlk;  // and chunk (lane / 16) + 4: bit 6 flipped
+          px[i].set(*reinterpret_cast<const u32x4_t*>(lds + o),
+                    *reinterpret_cast<const u32x4_t*>(lds + (o ^ 64u)),
                     sc[(wm * 64 + i * 16 + (lane & 15)) * 16]);
         }
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-          const uint32_t o = j * 16 * kBlk;
-          const uint8_t* const p = lds + ((uint32_t(ws - lds) + o) ^ flip);
-          Piece<EXACT> pw;
-          pw.set(*reinterpret_cast<const u32x4_t*>(ws + o), *reinterpret_cast<const u32x4_t*>(p),
-                 sw);
-#pragma unroll
-          for (int i = 0; i < FM; ++i) acc[j][i] = mfma_q8(pw, px[i], acc[j][i]);
+          const uint32_t o = wo + j * 16 * kBlk;
+          pw[j].set(*reinterpret_cast<const u32x4_t*>(lds + o),
+                    *reinterpret_cast<const u32x4_t*>(lds + (o ^ 64u)), sw);
         }
+#pragma unroll
+        for (int i = 0; i < FM; ++i) px[i].pin();
+#pragma unroll
+        for (int j = 0; j < FN; ++j) pw[j].pin();
       }
+      if (kt + 2 < KT) {
+        issue(kt + 2, st == 0 ? 2 : st - 1);
+        if ((kt & 15) == 0 && kt + 16 < KT) issue_scales((kt >> 4) + 1);
+        slot_wait<kMidLoadsX + kMidLoadsW>();
+      } else {
+        slot_wait<0>();
+      }
+      slot_barrier();
+      // matrix slot
+      if (active) {
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int i = 0; i < FM; ++i) mfma_q8(pw[j], px[i], acc[j][i]);
+        __builtin_amdgcn_s_setprio(0);
+      }
+      slot_barrier();
       st = st == 2 ? 0 : st + 1;
+    }
+    if (wm == 0) slot_barrier();
+    if (!EXACT) {
+      // what reads the accumulators comes after this
+      asm volatile("s_nop 15\n\ts_nop 15");
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int i = 0; i < FM; ++i) asm volatile("" : "+v"(acc[j][i]));
     }
 
     int drow[FM];
@@ -401,13 +495,19 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
     }
     const int c0 = cur.n0 + wn * 64 + 4 * (lane >> 4);
     if constexpr (KIND == kUp) {
+      const bool whole = cur.n0 + kMidTN <= a.Nout;
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
-        float top = 0.0f;
+        uint32_t top = 0;
 #pragma unroll
-        for (int j = 0; j < FN; ++j) top = fmaxf(top, hidden4<ACT>(acc[j][i], c0 + 16 * j, a.Nout));
-        top = fmaxf(top, __shfl_xor(top, 16, kWave));
-        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        for (int j = 0; j < FN; ++j)
+          top = max(top, hidden4<ACT>(acc[j][i], c0 + 16 * j, a.Nout, whole));
+        if (__builtin_expect(__any(top >= kInfBits), 0)) {
+          top = 0;
+#pragma unroll
+          for (int j = 0; j < FN; ++j) top = max(top, hidden_finite4<ACT>(acc[j][i]));
+        }
+        top = quad_max(top);
         if (lane < 16) s_top[wn][wm * 64 + i * 16 + lane] = top;
       }
       __syncthreads();
@@ -416,8 +516,8 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
       for (int i = 0; i < FM; ++i) {
         if (drow[i] < 0 || blk * kBlk >= a.qpitch) continue;
         const int row = wm * 64 + i * 16 + (lane & 15);
-        float top = fmaxf(s_top[wn & (kGated ? 0 : 2)][row], s_top[(wn & (kGated ? 0 : 2)) + 1][row]);
-        if (kGated) top = fmaxf(top, fmaxf(s_top[2][row], s_top[3][row]));
+        uint32_t top = max(s_top[wn & (kGated ? 0 : 2)][row], s_top[(wn & (kGated ? 0 : 2)) + 1][row]);
+        if (kGated) top = max(top, max(s_top[2][row], s_top[3][row]));
         const int byte = q8_scale_byte(top);
         const float inv = q8_inv(byte);
         if ((wn & (kGated ? 3 : 1)) == 0 && lane < 16)
@@ -440,6 +540,234 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
     if (!has_next) break;
     L = Ln;
     cur = nxt;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Tiles of TM = 128 or 64 rows by 128 columns (gated: 256 weight rows, TM = 64) in
+// blocks of four waves, two blocks per CU (gated: one): what one block waits for,
+// its loads, its conversions, its epilogue, runs beside the other's matrix
+// instructions.  Waves are 2 x 2 of 64 x 64 (TM = 128) or 1 x 4 of 64 x 32; a ring
+// of kStages k-tiles, one barrier each, in the swizzled order of the tile above,
+// scales in two buffers of 16 k-tiles.  A tile of TM = 64 skips the 16-row tiles
+// that it has no rows for.
+// ---------------------------------------------------------------------------
+template <int TM, bool GATED> struct Duo {
+  static constexpr int TN = GATED ? 256 : 128;
+  static constexpr int kWaves = 4, kThreads = kWaves * kWave;
+  static constexpr int kStages = TM == 128 ? 2 : 3;
+  static constexpr int kTileX = TM * kBlk, kStage = (TM + TN) * kBlk;
+  static constexpr int kLoadsX = TM / 8 / kWaves, kLoadsW = TN / 8 / kWaves;
+  static constexpr int kLoads = kLoadsX + kLoadsW;
+  static constexpr int kScales = (TM + TN / kBlk) * 16;
+  static constexpr int kBlocks = GATED ? 1 : 2;
+  static constexpr int kWavesM = TM / 64, kWavesN = kWaves / kWavesM;
+  static constexpr int FM = 4, FN = TN / kWavesN / 16;
+};
+
+template <int KIND, int ACT, typename T, bool EXACT, int TM>
+__global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qgemm_duo_kernel(
+    QArgs a) {
+  constexpr bool kGated = ACT == kActSwiglu;
+  typedef Duo<TM, kGated> D;
+  constexpr int FM = D::FM, FN = D::FN, WN = FN * 16;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[D::kStages * D::kStage];
+  __shared__ __attribute__((aligned(16))) uint8_t s_sc[2][D::kScales];
+  __shared__ int s_src[TM], s_dst[TM];
+  __shared__ uint32_t s_top[KIND == kUp ? D::kWavesN : 1][TM];
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wv / D::kWavesN, wn = wv % D::kWavesN;
+  const int nt = (a.Nout + D::TN - 1) / D::TN;
+  const int total = KIND == kDense ? (a.M + TM - 1) / TM * nt : a.tile_off[a.G];
+  const int per = (total + kXcds - 1) / kXcds;
+  const int lo = (blockIdx.x % kXcds) * per;
+  const int hi = min(total, lo + per);
+  const int stride = gridDim.x / kXcds;
+  int toff0 = 0, toff1 = 0;
+  if constexpr (KIND != kDense) {
+    toff0 = lane < a.G ? a.tile_off[lane] : 0x7fffffff;
+    toff1 = lane + 64 < a.G ? a.tile_off[lane + 64] : 0x7fffffff;
+  }
+  const int KT = a.pitch / kBlk;
+  const int nbw = (a.Nout + kBlk - 1) / kBlk;
+  const int chunk = (lane & 7) ^ (4 * (wv & 1) + (lane >> 4));
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(lds) + wv * 1024);
+  const uint32_t sc0 = __builtin_amdgcn_readfirstlane(lds_addr(&s_sc[0][0]) + wv * 1024);
+  const uint32_t fr = (lane & 15) * kBlk + (((lane >> 4) ^ ((lane >> 1) & 7)) * 16);
+
+  for (int L = lo + static_cast<int>(blockIdx.x) / kXcds; L < hi; L += stride) {
+    int e = 0, e_base = 0, o0 = 0, cnt = a.M;
+    if constexpr (KIND != kDense) {
+      e = tile_group(L, toff0, toff1, e_base);
+      o0 = a.off[e];
+      cnt = a.off[e + 1] - o0;
+    }
+    const int mt = (cnt + TM - 1) / TM;
+    int m, n;
+    band_order(L - e_base, mt, nt, m, n);
+    e = __builtin_amdgcn_readfirstlane(e);
+    const int r0 = __builtin_amdgcn_readfirstlane(o0 + m * TM);
+    const int rows = __builtin_amdgcn_readfirstlane(min(TM, cnt - m * TM));
+    const int n0 = __builtin_amdgcn_readfirstlane(n * D::TN);
+    const bool routed = KIND == kDense || e < a.E;
+    const int64_t g = routed ? e : e - a.E;
+    const uint8_t* const W = (routed ? a.W : a.Wsh) + g * a.Nout * a.pitch;
+    const uint8_t* const Ws = (routed ? a.Ws : a.Wssh) + g * nbw * a.spitch;
+    const uint8_t *gx[D::kLoadsX], *gw[D::kLoadsW], *gs;
+#pragma unroll
+    for (int u = 0; u < D::kLoadsW; ++u)
+      gw[u] = W + int64_t(min(n0 + 8 * (wv + D::kWaves * u) + (lane >> 3), a.Nout - 1)) * a.pitch +
+              chunk * 16;
+    auto issue_w = [&](int kt, int st) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < D::kLoadsW; ++u)
+        dma16(reinterpret_cast<const uint16_t*>(gw[u] + int64_t(kt) * kBlk),
+              lds0 + st * D::kStage + D::kTileX + u * D::kWaves * 1024);
+    };
+    auto issue_x = [&](int kt, int st) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < D::kLoadsX; ++u)
+        dma16(reinterpret_cast<const uint16_t*>(gx[u] + int64_t(kt) * kBlk),
+              lds0 + st * D::kStage + u * D::kWaves * 1024);
+    };
+    // scales: the rows' by the first waves, the weight blocks' by the last
+    auto issue_scales = [&](int c) __attribute__((always_inline)) {
+      const uint32_t to = __builtin_amdgcn_readfirstlane(sc0 + (c & 1) * D::kScales);
+      if (wv < TM / 64) dma16(reinterpret_cast<const uint16_t*>(gs + c * 16), to);
+      if (wv == TM / 64 && lane < D::TN / kBlk)
+        dma16(reinterpret_cast<const uint16_t*>(gs + c * 16), __builtin_amdgcn_readfirstlane(to));
+    };
+    // the weights need no row table: their first k-tiles are asked for before it
+    issue_w(0, 0);
+    if (tid < TM) {
+      int src, dst;
+      tile_row<KIND>(a, e, r0, rows, tid, src, dst);
+      s_src[tid] = src;
+      s_dst[tid] = dst;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < D::kLoadsX; ++u)
+      gx[u] = a.X + int64_t(s_src[8 * (wv + D::kWaves * u) + (lane >> 3)]) * a.pitch + chunk * 16;
+    gs = wv < TM / 64 ? a.Xs + int64_t(s_src[(64 * wv + lane) & (TM - 1)]) * a.spitch
+                      : Ws + int64_t(min(n0 / kBlk + (lane & 1), nbw - 1)) * a.spitch;
+    issue_scales(0);
+    issue_x(0, 0);
+    if (D::kStages > 2 && KT > 1) {
+      issue_w(1, 1);
+      issue_x(1, 1);
+    }
+
+    f32x4_t acc[FN][FM];
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int i = 0; i < FM; ++i) acc[j][i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    // the k-loop for a wave with NI 16-row tiles
+    auto run = [&](auto ni_c) __attribute__((always_inline)) {
+      constexpr int NI = decltype(ni_c)::value;
+      int st = 0;
+      for (int kt = 0; kt < KT; ++kt) {
+        if (D::kStages > 2 && kt + 1 < KT) slot_wait<D::kLoads>();
+        else slot_wait<0>();
+        slot_barrier();
+        constexpr int kAhead = D::kStages - 1;
+        if (kt + kAhead < KT) {
+          const int to = st + kAhead >= D::kStages ? st + kAhead - D::kStages : st + kAhead;
+          issue_w(kt + kAhead, to);
+          issue_x(kt + kAhead, to);
+          if ((kt & 15) == 0 && kt + 16 < KT) issue_scales((kt >> 4) + 1);
+        }
+        if constexpr (NI > 0) {
+          const uint32_t xo = st * D::kStage + wm * 64 * kBlk + fr;
+          const uint32_t wo = st * D::kStage + D::kTileX + wn * WN * kBlk + fr;
+          const uint8_t* const sc = s_sc[(kt >> 4) & 1] + (kt & 15);
+          const int sw = sc[(TM + (wn * WN) / kBlk) * 16];
+          Piece<EXACT> px[NI > 0 ? NI : 1];
+#pragma unroll
+          for (int i = 0; i < NI; ++i) {
+            const uint32_t o = xo + i * 16 * kBlk;
+            px[i].set(*reinterpret_cast<const u32x4_t*>(lds + o),
+                      *reinterpret_cast<const u32x4_t*>(lds + (o ^ 64u)),
+                      sc[(wm * 64 + i * 16 + (lane & 15)) * 16]);
+          }
+#pragma unroll
+          for (int j = 0; j < FN; ++j) {
+            const uint32_t o = wo + j * 16 * kBlk;
+            Piece<EXACT> pw;
+            pw.set(*reinterpret_cast<const u32x4_t*>(lds + o),
+                   *reinterpret_cast<const u32x4_t*>(lds + (o ^ 64u)), sw);
+#pragma unroll
+            for (int i = 0; i < NI; ++i) mfma_q8(pw, px[i], acc[j][i]);
+          }
+        }
+        st = st + 1 == D::kStages ? 0 : st + 1;
+      }
+    };
+    const int mine = rows - wm * 64;
+    if (n0 + wn * WN >= a.Nout || mine <= 0) run(std::integral_constant<int, 0>{});
+    else if (TM == 64 && mine <= 16) run(std::integral_constant<int, 1>{});
+    else if (TM == 64 && mine <= 32) run(std::integral_constant<int, 2>{});
+    else run(std::integral_constant<int, 4>{});
+    if (!EXACT) {
+      asm volatile("s_nop 15\n\ts_nop 15");
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int i = 0; i < FM; ++i) asm volatile("" : "+v"(acc[j][i]));
+    }
+
+    const int c0 = n0 + wn * WN + 4 * (lane >> 4);
+    if constexpr (KIND == kUp) {
+      const bool whole = n0 + D::TN <= a.Nout;
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        if (TM == 64 && i * 16 >= rows) continue;
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          top = max(top, hidden4<ACT>(acc[j][i], c0 + 16 * j, a.Nout, whole));
+        if (__builtin_expect(__any(top >= kInfBits), 0)) {
+          top = 0;
+#pragma unroll
+          for (int j = 0; j < FN; ++j) top = max(top, hidden_finite4<ACT>(acc[j][i]));
+        }
+        top = quad_max(top);
+        if (lane < 16) s_top[wn][wm * 64 + i * 16 + lane] = top;
+      }
+      __syncthreads();
+      const int blk = (kGated ? n0 / 2 : n0) / kBlk;
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const int row = wm * 64 + i * 16 + (lane & 15);
+        const int64_t drow = s_dst[row];
+        if (drow < 0) continue;
+        uint32_t top = s_top[0][row];
+#pragma unroll
+        for (int w = 1; w < D::kWavesN; ++w) top = max(top, s_top[w][row]);
+        const int byte = q8_scale_byte(top);
+        const float inv = q8_inv(byte);
+        if (wn == 0 && lane < 16) a.s[drow * a.qspitch + blk] = static_cast<uint8_t>(byte);
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          store_hidden4<ACT>(a.q + drow * a.qpitch, c0 + 16 * j, acc[j][i], inv);
+      }
+    } else {
+      T* const og = static_cast<T*>(routed ? a.dst : a.dst_sh);
+      const bool vec = (reinterpret_cast<uintptr_t>(og) & 15u) == 0 && a.ldo % 4 == 0;
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const int64_t drow = s_dst[wm * 64 + i * 16 + (lane & 15)];
+        if (drow < 0) continue;
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          store_out4(a, og + drow * a.ldo, c0 + 16 * j, acc[j][i], vec);
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -473,37 +801,6 @@ constexpr int kTallBuf = 4 * kTallHalf;  // X0 X1 W0 W1
 constexpr int kTallMinKT = 4;            // k-tiles
 constexpr int kTallScales = (kTallTM + 2) * 16;
 
-__device__ __forceinline__ void tall_barrier() {
-  __builtin_amdgcn_sched_barrier(0);
-  asm volatile("s_barrier" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
-}
-
-// One wait for both: at most N loads of this wave in flight (N < 16), every LDS
-// read returned.
-template <int N>
-__device__ __forceinline__ void tall_wait() {
-  __builtin_amdgcn_sched_barrier(0);
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(N) : "memory");
-  __builtin_amdgcn_sched_barrier(0);
-}
-
-// c += w x with the accumulator in place.  The builtin leaves the compiler free to
-// put the sum elsewhere and to move the instruction past branches, barriers and
-// waits; with 128 accumulator registers of 256 that ended in spills between the
-// loads of the ring.  The operands' LDS reads are waited for by the caller
-// (tall_wait), two wait states follow any vector instruction that wrote one, each
-// accumulator is used once between two barriers, and the epilogue's first read is
-// held off (below): the distances that the hardware leaves to the program.
-__device__ __forceinline__ void mfma_q8_tied(f32x4_t& c, const i32x8_t& w, const i32x8_t& x,
-                                             int sw, int sx) {
-  asm volatile(
-      "s_nop 1\n\t"
-      "v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]"
-      : "+v"(c)
-      : "v"(w), "v"(x), "v"(sw), "v"(sx));
-}
-
 template <int KIND, int ACT, typename T>
 __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
   constexpr bool kGated = ACT == kActSwiglu;
@@ -513,7 +810,7 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t s_sc[3 * kTallScales];
   __shared__ int s_list[2][kTallTM];
   __shared__ int s_toff[128];
-  __shared__ float s_top[KIND == kUp ? 2 : 1][4][kTallTM];
+  __shared__ uint32_t s_top[KIND == kUp ? 2 : 1][4][kTallTM];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -557,11 +854,11 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
       cnt = a.off[t.e + 1] - o0;
     }
     const int mt = (cnt + TM - 1) / TM;
-    const int local = __builtin_amdgcn_readfirstlane(L - e_base);
-    const int m = local % mt;
+    int m, n;
+    band_order(__builtin_amdgcn_readfirstlane(L - e_base), mt, nt, m, n);
     t.r0 = __builtin_amdgcn_readfirstlane(o0 + static_cast<int>(int64_t(m) * cnt / mt));
     t.rows = __builtin_amdgcn_readfirstlane(o0 + static_cast<int>(int64_t(m + 1) * cnt / mt) - t.r0);
-    t.n0 = __builtin_amdgcn_readfirstlane((local / mt) * kTallTN);
+    t.n0 = __builtin_amdgcn_readfirstlane(n * kTallTN);
     return t;
   };
 
@@ -664,8 +961,8 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
   int lb = 0, sb = 0;      // row table and first buffer of the tile
   int sc = 0;              // scale buffer of the k-tile (0, 1, 2)
   if (kListed) fetch_list(cur, 0);
-  tall_wait<0>();
-  tall_barrier();
+  slot_wait<0>();
+  slot_barrier();
   aim(cur, 0);
   issue_scales(cur, 0, 0, 0);
 #pragma unroll
@@ -675,12 +972,12 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
     issue_w(p, p, 1);
     issue_x(p, p, 1, kTallTM);
   }
-  tall_wait<0>();
-  tall_barrier();
+  slot_wait<0>();
+  slot_barrier();
   read_w(fa, 0, 0);
-  tall_wait<0>();
-  tall_barrier();
-  if (wm == 1) tall_barrier();
+  slot_wait<0>();
+  slot_barrier();
+  if (wm == 1) slot_barrier();
 
   f32x4_t acc[4][8];  // [column tile][row tile]
   for (;;) {
@@ -714,8 +1011,8 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
         constexpr int nx = kTail || NX == 4 ? 256 : NX == 2 ? 192 : 128;
         const int so = __builtin_amdgcn_readfirstlane(sc * kTallScales + (t & 15));
         auto settle = [&]() __attribute__((always_inline)) {
-          tall_wait<kTail ? 8 : 8 + NX>();
-          tall_barrier();
+          slot_wait<kTail ? 8 : 8 + NX>();
+          slot_barrier();
         };
         // phase 0: X0 x W0
         read_x(b, 0, 4);
@@ -725,13 +1022,13 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
         issue_w(lt, b, 0);
         settle();
         mfma_q(0, 0, p, sw0);
-        tall_barrier();
+        slot_barrier();
         // phase 1: X0 x W1
         if (CA) read_w(q, b, 1);
         issue_x(lt, b, 0, nx);
         settle();
         if (CA) mfma_q(0, 1, q, sw1);
-        tall_barrier();
+        slot_barrier();
         // phase 2: X1 x W1
         if (NX > 0) {
           read_x(b, 1, NX);
@@ -740,13 +1037,13 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
         issue_w(lt, b, 1);
         settle();
         if (CA && NX > 0) mfma_q(1, 1, q, sw1);
-        tall_barrier();
+        slot_barrier();
         // phase 3: X1 x W0, and the next k-tile's W0
         read_w(q, b ^ 1, 0);
         issue_x(lt, b, 1, nx);
         settle();
         if (NX > 0) mfma_q(1, 0, p, sw0);
-        tall_barrier();
+        slot_barrier();
       };
       // No branches inside a k-tile: tables and scales are asked for between them,
       // and the last tile's last two k-tiles load as the others' do (its own first
@@ -807,26 +1104,28 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
     const int lane = fresh_lane();
     const int g = lane >> 4, odd = g & 1;
     if constexpr (KIND == kUp) {
+      const bool whole = cur.n0 + kTallTN <= a.Nout;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int row = 128 * (i >> 2) + 16 * (2 * (i & 3) + wm) + (lane & 15);
-        float top[2];
+        uint32_t top[2];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const int c0 = cur.n0 + 128 * c + 32 * wn + 4 * g;
-          top[c] = fmaxf(hidden4<ACT>(acc[2 * c][i], c0, a.Nout),
-                         hidden4<ACT>(acc[2 * c + 1][i], c0 + 16, a.Nout));
+          top[c] = max(hidden4<ACT>(acc[2 * c][i], c0, a.Nout, whole),
+                       hidden4<ACT>(acc[2 * c + 1][i], c0 + 16, a.Nout, whole));
+          if (__builtin_expect(__any(top[c] >= kInfBits), 0))
+            top[c] = max(hidden_finite4<ACT>(acc[2 * c][i]), hidden_finite4<ACT>(acc[2 * c + 1][i]));
         }
-        if (kGated) top[0] = fmaxf(top[0], top[1]);
+        if (kGated) top[0] = max(top[0], top[1]);
 #pragma unroll
         for (int c = 0; c < (kGated ? 1 : 2); ++c) {
-          top[c] = fmaxf(top[c], __shfl_xor(top[c], 16, kWave));
-          top[c] = fmaxf(top[c], __shfl_xor(top[c], 32, kWave));
+          top[c] = quad_max(top[c]);
           if (lane < 16) s_top[c][wn][row] = top[c];
         }
       }
-      tall_wait<15>();
-      tall_barrier();
+      slot_wait<15>();
+      slot_barrier();
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int row = 128 * (i >> 2) + 16 * (2 * (i & 3) + wm) + (lane & 15);
@@ -838,8 +1137,8 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
           const int blk = kGated ? cur.n0 / 2 / kBlk : cur.n0 / kBlk + c;
           if (blk * kBlk >= a.qpitch) continue;
           const int tc = kGated ? 0 : c;
-          const int byte = q8_scale_byte(fmaxf(fmaxf(s_top[tc][0][row], s_top[tc][1][row]),
-                                               fmaxf(s_top[tc][2][row], s_top[tc][3][row])));
+          const int byte = q8_scale_byte(max(max(s_top[tc][0][row], s_top[tc][1][row]),
+                                             max(s_top[tc][2][row], s_top[tc][3][row])));
           const float inv = q8_inv(byte);
           if (wn == 0 && lane < 16 && (!kGated || c == 0))
             a.s[drow * a.qspitch + blk] = static_cast<uint8_t>(byte);
@@ -907,8 +1206,8 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
     cur = nxt;
     lb ^= 1;
   }
-  if (wm == 0) tall_barrier();
-  tall_wait<0>();  // the last loads have landed before the LDS is given up
+  if (wm == 0) slot_barrier();
+  slot_wait<0>();  // the last loads have landed before the LDS is given up
 }
 
 template <int KIND, int ACT, typename T, bool EXACT>
@@ -925,11 +1224,22 @@ hipError_t launch_tall(const QArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <int KIND, int ACT, typename T, bool EXACT, int TM>
+hipError_t launch_duo(const QArgs& a, hipStream_t st) {
+  launch_kernel(&qgemm_duo_kernel<KIND, ACT, T, EXACT, TM>,
+                dim3(device_cus() * Duo<TM, ACT == kActSwiglu>::kBlocks), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
 template <int ACT>
-hipError_t launch_up(const QArgs& a, bool exact, bool tall, hipStream_t st) {
-  if (tall) return launch_tall<kUp, ACT, float>(a, st);
-  if (exact) return launch<kUp, ACT, float, true>(a, st);
-  return launch<kUp, ACT, float, false>(a, st);
+hipError_t launch_up(const QArgs& a, bool exact, const FfnPlan& plan, hipStream_t st) {
+  if (plan.tall_up) return launch_tall<kUp, ACT, float>(a, st);
+  if (plan.tm_up == 64) return launch_duo<kUp, ACT, float, true, 64>(a, st);
+  if constexpr (ACT == kActSwiglu)
+    return exact ? launch<kUp, ACT, float, true>(a, st) : launch<kUp, ACT, float, false>(a, st);
+  else
+    return exact ? launch_duo<kUp, ACT, float, true, 128>(a, st)
+                 : launch_duo<kUp, ACT, float, false, 128>(a, st);
 }
 
 // Whether the 256 x 256 tiles can take a product: rows addressed by 32-bit byte
@@ -958,11 +1268,18 @@ FfnPlan q8_plan(const Shape& s, StepKind kind, int64_t rows) {
   FfnPlan p;
   p.tm = p.tm_up = kMidTM;
   p.tn_up = p.tn_down = kMidTN;
-  const bool many = rows / s.E >= 144;
+  const bool many = rows / s.E >= 144, few = rows / s.E <= 48;
   p.tall_up = many && !exact_up(s) && tall_capable(s.tokens(), s.d);
   p.tall_down = many && s.bf16 && tall_capable(s.mid_rows(), s.d_ff);
   if (p.tall_up) p.tm_up = kTallTM;
   if (p.tall_down) p.tm = kTallTM;
+  if (few) {
+    p.tm_up = p.tm = 64;
+    p.tn_down = 128;
+    if (!s.swiglu) p.tn_up = 128;
+  } else if (!s.swiglu && !p.tall_up) {
+    p.tn_up = 128;
+  }
   return p;
 }
 
@@ -992,9 +1309,9 @@ hipError_t launch_q8_up(const Shape& s, int act, const FfnPlan& plan, const Quan
   a.qspitch = static_cast<int>(q8_spitch(s.d_ff));
   a.tm = b.tiles + 2 * (s.groups() + 1);
   const bool exact = exact_up(s);
-  if (act == MOECA_ACT_SWIGLU) return launch_up<kActSwiglu>(a, exact, plan.tall_up, st);
-  if (act == MOECA_ACT_GELU_ERF) return launch_up<kActGeluErf>(a, exact, plan.tall_up, st);
-  return launch_up<kActGeluTanh>(a, exact, plan.tall_up, st);
+  if (act == MOECA_ACT_SWIGLU) return launch_up<kActSwiglu>(a, exact, plan, st);
+  if (act == MOECA_ACT_GELU_ERF) return launch_up<kActGeluErf>(a, exact, plan, st);
+  return launch_up<kActGeluTanh>(a, exact, plan, st);
 }
 
 hipError_t launch_q8_down(const Shape& s, const FfnPlan& plan, const QuantWeights& w,
@@ -1022,6 +1339,9 @@ hipError_t launch_q8_down(const Shape& s, const FfnPlan& plan, const QuantWeight
   a.dst_sh = b.h_sh;
   a.tm = b.tiles + 2 * (s.groups() + 1) + 1;
   if (plan.tall_down) return launch_tall<kDown, kActNone, uint16_t>(a, st);
+  if (plan.tm == 64)
+    return s.bf16 ? launch_duo<kDown, kActNone, uint16_t, true, 64>(a, st)
+                  : launch_duo<kDown, kActNone, float, true, 64>(a, st);
   if (s.bf16) return launch<kDown, kActNone, uint16_t, false>(a, st);
   return launch<kDown, kActNone, float, true>(a, st);
 }
@@ -1045,8 +1365,12 @@ hipError_t launch_q8_linear(const Q8& x, int64_t M, int K, const void* W, const 
     a.dense_tm = tall_rows_one(M, (N + kTallTN - 1) / kTallTN, device_cus());
     return launch_tall<kDense, kActNone, uint16_t>(a, st);
   }
+  // tiles of 64 rows where those of 128 leave CUs without one
+  if ((M + 127) / 128 * ((N + 255) / 256) < device_cus())
+    return bf16 ? launch_duo<kDense, kActNone, uint16_t, true, 64>(a, st)
+                : launch_duo<kDense, kActNone, float, true, 64>(a, st);
   if (bf16) return launch<kDense, kActNone, uint16_t, false>(a, st);
-  return launch<kDense, kActNone, float, true>(a, st);
+  return launch_duo<kDense, kActNone, float, true, 128>(a, st);
 }
 
 }  // namespace moeca

@@ -88,7 +88,7 @@ template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void quant_matrix_kernel(const T* __restrict__ W, int N, int K,
                                                            uint8_t* __restrict__ q,
                                                            uint8_t* __restrict__ s) {
-  __shared__ float s_top[4];
+  __shared__ uint32_t s_top[4];
   const int pitch = static_cast<int>(q8_pitch(K)), spitch = static_cast<int>(q8_spitch(K));
   const int nb = (N + kBlk - 1) / kBlk;
   const int kb = blockIdx.x, n0 = blockIdx.y * kBlk;
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256) void quant_matrix_kernel(const T* __restrict__
   const int tid = threadIdx.x;
   const int c = kb * kBlk + (tid & 15) * 8;
   float v[8][8];
-  float top = 0.0f;
+  uint32_t top = 0;
 #pragma unroll
   for (int h = 0; h < 8; ++h) {
     const int n = n0 + (tid >> 4) + 16 * h;
@@ -107,14 +107,14 @@ __global__ __launch_bounds__(256) void quant_matrix_kernel(const T* __restrict__
       for (int u = 0; u < 8; ++u) v[h][u] = 0.0f;
     }
 #pragma unroll
-    for (int u = 0; u < 8; ++u) top = fmaxf(top, q8_mag(v[h][u]));
+    for (int u = 0; u < 8; ++u) top = max(top, q8_finite(v[h][u]));
   }
-  top = row_max_f32(top);
-  top = fmaxf(top, __shfl_xor(top, 16, kWave));
-  top = fmaxf(top, __shfl_xor(top, 32, kWave));
+  top = row_max_u32(top);
+  top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 16, kWave)));
+  top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32, kWave)));
   if ((tid & (kWave - 1)) == 0) s_top[tid / kWave] = top;
   __syncthreads();
-  top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+  top = max(max(s_top[0], s_top[1]), max(s_top[2], s_top[3]));
   const int byte = q8_scale_byte(top);
   const float inv = q8_inv(byte);
   if (tid == 0) s[(i * nb + blockIdx.y) * spitch + kb] = static_cast<uint8_t>(byte);

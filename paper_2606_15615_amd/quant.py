@@ -10,45 +10,60 @@ unless one is given.
 """
 from __future__ import annotations
 
+import torch
+
 from . import _lib
-from .layer import _torch
+
+_BF16, _FP32 = torch.bfloat16, torch.float32
+_CODE = {_BF16: _lib.MOECA_DTYPE_BF16, _FP32: _lib.MOECA_DTYPE_FP32}
 
 
 def _dtype(t):
-    torch = _torch()
-    if t.dtype == torch.bfloat16:
-        return _lib.MOECA_DTYPE_BF16
-    if t.dtype == torch.float32:
-        return _lib.MOECA_DTYPE_FP32
-    raise TypeError(f"rows are bfloat16 or float32, not {t.dtype}")
+    code = _CODE.get(t.dtype)
+    if code is None:
+        raise TypeError(f"rows are bfloat16 or float32, not {t.dtype}")
+    return code
 
 
-def _on(device, stream):
-    """The device's guard, and the stream to enqueue on."""
-    torch = _torch()
-    s = stream if stream is not None else torch.cuda.current_stream(device)
-    return torch.cuda.device(device), s.cuda_stream
+def _launch(fn, device, stream, *args):
+    """Call ``fn(*args, stream)`` of the library with the device current.  (A call of
+    a few microseconds: the guard is entered only where another device is current,
+    and the current stream's handle is asked for without making an object of it.)"""
+    index = device.index
+    if index is None or device.type != "cuda":
+        raise ValueError(f"the tensors are on {device}, not on a GPU")
+    raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if torch.cuda.current_device() == index:
+        rc = fn(*args, raw)
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, raw)
+    if rc != _lib.MOECA_OK:
+        _lib._check(rc)
 
 
 def _rows(t, width, device, what):
     """(pointer, rows, row stride) of a 2-d tensor of the activation type."""
-    if t.ndim != 2 or t.shape[1] != width:
-        raise ValueError(f"{what}: expected rows of width {width}, got {tuple(t.shape)}")
+    shape = t.shape
+    if len(shape) != 2 or shape[1] != width:
+        raise ValueError(f"{what}: expected rows of width {width}, got {tuple(shape)}")
     if t.device != device:
         raise ValueError(f"{what} is on {t.device}, expected {device}")
-    if t.shape[0] > 0 and width > 1 and t.stride(1) != 1:
+    rows = shape[0]
+    ld, inner = t.stride()
+    if rows > 0 and width > 1 and inner != 1:
         raise ValueError(f"{what}: the elements of a row must be contiguous")
-    ld = t.stride(0) if t.shape[0] > 1 else width
+    if rows <= 1:
+        ld = width
     if ld < width:
         raise ValueError(f"{what}: rows overlap (stride {ld}, width {width})")
-    return t.data_ptr() or None, t.shape[0], ld
+    return t.data_ptr() or None, rows, ld
 
 
 def _indexes(slot, rows, device):
     if slot is None:
         return None
-    torch = _torch()
-    if slot.dtype != torch.int32 or slot.ndim != 1 or not slot.is_contiguous():
+    if slot.dtype != torch.int32 or slot.dim() != 1 or not slot.is_contiguous():
         raise ValueError("slots are a contiguous int32 vector")
     if slot.device != device:
         raise ValueError(f"slots are on {slot.device}, expected {device}")
@@ -59,7 +74,6 @@ def _indexes(slot, rows, device):
 
 def _bytes(t, shape, what):
     """A dense 8-bit tensor of this shape, as uint8."""
-    torch = _torch()
     if t.element_size() != 1 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
         raise ValueError(f"{what}: expected contiguous bytes of shape {tuple(shape)}, "
                          f"got {t.dtype} {tuple(t.shape)}")
@@ -72,10 +86,10 @@ class QuantRows:
     start as zeros."""
 
     def __init__(self, slots, K, *, device="cuda:0", q=None, scale=None, norm=False):
-        torch = _torch()
         self.slots, self.K = int(slots), int(K)
         if self.slots < 0 or self.K < 1:
             raise ValueError("slots must be >= 0 and K >= 1")
+        self._lib = _lib.load()
         self.pitch, self.scale_pitch = _lib.moeca_quant_pitch(K), _lib.moeca_quant_scale_pitch(K)
         if (q is None) != (scale is None):
             raise ValueError("q and scale come together")
@@ -83,6 +97,7 @@ class QuantRows:
             q = torch.zeros(self.slots, self.pitch, dtype=torch.uint8, device=device)
             scale = torch.zeros(self.slots, self.scale_pitch, dtype=torch.uint8, device=device)
         self.q = _bytes(q, (self.slots, self.pitch), "q")
+        self.device = self.q.device
         self.scale = _bytes(scale, (self.slots, self.scale_pitch), "scale")
         if norm is True:
             norm = torch.zeros(self.slots, device=self.q.device)
@@ -98,35 +113,30 @@ class QuantRows:
     def write(self, x, slot=None, stream=None):
         """Quantise the rows of ``x`` [rows][K] into ``slot`` (int32, default row r into
         slot r); a slot outside the range leaves its row out."""
-        p, rows, ld = _rows(x, self.K, self.q.device, "x")
-        at = _indexes(slot, rows, self.q.device)
+        p, rows, ld = _rows(x, self.K, self.device, "x")
+        at = _indexes(slot, rows, self.device)
         if rows == 0:
             return
-        dev, st = _on(self.q.device, stream)
-        with dev:
-            _lib.moeca_quant_rows(p, _dtype(x), rows, self.K, ld, at, self.slots,
-                                  self.q.data_ptr(), self.scale.data_ptr(),
-                                  None if self.norm is None else self.norm.data_ptr(), st)
+        _launch(self._lib.moeca_quant_rows, self.device, stream, p, _dtype(x), rows, self.K, ld,
+                at, self.slots, self.q.data_ptr(), self.scale.data_ptr(),
+                None if self.norm is None else self.norm.data_ptr())
 
     def read(self, slot=None, dtype=None, out=None, stream=None):
         """The values of rows ``slot`` (default: all), in ``out`` or a new tensor of
         ``dtype`` (bfloat16); a slot outside the range gives zeros."""
-        torch = _torch()
-        at = _indexes(slot, None, self.q.device)
+        at = _indexes(slot, None, self.device)
         rows = self.slots if slot is None else slot.shape[0]
         if out is None:
-            out = torch.empty(rows, self.K, dtype=dtype or torch.bfloat16, device=self.q.device)
+            out = torch.empty(rows, self.K, dtype=dtype or _BF16, device=self.device)
         elif dtype is not None and out.dtype != dtype:
             raise TypeError(f"out is {out.dtype}, not {dtype}")
-        p, n, ld = _rows(out, self.K, self.q.device, "out")
+        p, n, ld = _rows(out, self.K, self.device, "out")
         if n != rows:
             raise ValueError(f"out has {n} rows for {rows}")
         if rows == 0:
             return out
-        dev, st = _on(self.q.device, stream)
-        with dev:
-            _lib.moeca_dequant_rows(self.q.data_ptr(), self.scale.data_ptr(), self.slots, self.K,
-                                    at, rows, p, _dtype(out), ld, st)
+        _launch(self._lib.moeca_dequant_rows, self.device, stream, self.q.data_ptr(),
+                self.scale.data_ptr(), self.slots, self.K, at, rows, p, _dtype(out), ld)
         return out
 
 
@@ -135,6 +145,7 @@ class QuantMatrix:
     [n][N][pitch], ``scale`` [n][ceil(N / 128)][scale pitch] (one matrix: without n)."""
 
     def __init__(self, q, scale, N, K):
+        self._lib = _lib.load()
         self.N, self.K = int(N), int(K)
         lead = tuple(q.shape[:-2])
         if len(lead) > 1:
@@ -142,13 +153,13 @@ class QuantMatrix:
         self.q = _bytes(q, lead + (self.N, _lib.moeca_quant_pitch(K)), "q")
         self.scale = _bytes(scale, lead + (-(-self.N // 128), _lib.moeca_quant_scale_pitch(K)),
                             "scale")
-        if self.scale.device != self.q.device:
+        self.device = self.q.device
+        if self.scale.device != self.device:
             raise ValueError("q and scale must be on one device")
 
 
 def quantize_matrix(W, stream=None) -> QuantMatrix:
     """Quantise W [N][K], or a stack [n][N][K], bfloat16 or float32."""
-    torch = _torch()
     if W.ndim not in (2, 3) or not W.is_contiguous():
         raise ValueError("W is a contiguous [N][K] or [n][N][K] tensor")
     N, K = W.shape[-2:]
@@ -156,16 +167,13 @@ def quantize_matrix(W, stream=None) -> QuantMatrix:
     q = torch.empty(lead + (N, _lib.moeca_quant_pitch(K)), dtype=torch.uint8, device=W.device)
     s = torch.zeros(lead + (-(-N // 128), _lib.moeca_quant_scale_pitch(K)), dtype=torch.uint8,
                     device=W.device)
-    dev, st = _on(W.device, stream)
-    with dev:
-        _lib.moeca_quant_matrix(W.data_ptr(), _dtype(W), lead[0] if lead else 1, N, K,
-                                q.data_ptr(), s.data_ptr(), st)
+    _launch(_lib.load().moeca_quant_matrix, W.device, stream, W.data_ptr(), _dtype(W),
+            lead[0] if lead else 1, N, K, q.data_ptr(), s.data_ptr())
     return QuantMatrix(q, s, N, K)
 
 
 def linear_workspace(M, K, device="cuda:0"):
     """A workspace for ``linear`` calls of up to M rows of width K, one at a time."""
-    torch = _torch()
     return torch.empty(_lib.moeca_quant_linear_bytes(M, K), dtype=torch.uint8, device=device)
 
 
@@ -174,10 +182,9 @@ def linear(x, W: QuantMatrix, bias=None, out=None, workspace=None, stream=None):
     and one quantised matrix; ``out`` [M][N] is of x's type.  Without a
     ``workspace`` one is allocated for the call, which then has to run on the
     current stream."""
-    torch = _torch()
     if W.q.ndim != 2:
         raise ValueError("linear takes one matrix, not a stack")
-    device = W.q.device
+    device = W.device
     px, M, ldx = _rows(x, W.K, device, "x")
     dt = _dtype(x)
     if out is None:
@@ -198,10 +205,7 @@ def linear(x, W: QuantMatrix, bias=None, out=None, workspace=None, stream=None):
         workspace = linear_workspace(M, W.K, device)
     elif workspace.device != device or not workspace.is_contiguous():
         raise ValueError(f"workspace: expected contiguous bytes on {device}")
-    dev, st = _on(device, stream)
-    with dev:
-        _lib.moeca_quant_linear(px, dt, M, W.K, ldx, W.q.data_ptr(), W.scale.data_ptr(), W.N,
-                                None if bias is None else bias.data_ptr(), po, ldo,
-                                workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                st)
+    _launch(W._lib.moeca_quant_linear, device, stream, px, dt, M, W.K, ldx, W.q.data_ptr(),
+            W.scale.data_ptr(), W.N, None if bias is None else bias.data_ptr(), po, ldo,
+            workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return out

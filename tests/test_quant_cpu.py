@@ -231,3 +231,19 @@ def test_python_refusals():
     assert quant.linear(torch.zeros(0, 200), W).shape == (0, 70)
     with pytest.raises(ValueError, match="contiguous"):
         quant.quantize_matrix(torch.zeros(8, 4).T)
+
+
+def test_host_tensors_are_refused():
+    import torch
+    from paper_2606_15615_amd import quant
+    r = quant.QuantRows(3, 20, device="cpu")
+    with pytest.raises(ValueError, match="not on a GPU"):
+        r.write(torch.zeros(2, 20))
+    with pytest.raises(ValueError, match="not on a GPU"):
+        r.read()
+    with pytest.raises(ValueError, match="not on a GPU"):
+        quant.quantize_matrix(torch.zeros(2, 20))
+    W = quant.QuantMatrix(torch.zeros(70, 256, dtype=torch.uint8),
+                          torch.zeros(1, 16, dtype=torch.uint8), 70, 200)
+    with pytest.raises(ValueError, match="not on a GPU"):
+        quant.linear(torch.zeros(1, 200), W)
