@@ -120,30 +120,32 @@ __device__ __forceinline__ uint32_t pack2_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_q{a, b}, bf16x2_q));
 }
 
-// Four consecutive outputs of a row from column c on; whole: all four exist and
-// the address is a multiple of their size.
-template <typename T>
-__device__ __forceinline__ void store4(T* p, f32x4_t v, int n, bool whole) {
-  if (whole) {
-    if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<u32x2_t*>(p) =
-          u32x2_t{f32_to_bf16(v[0]) | (uint32_t(f32_to_bf16(v[1])) << 16),
-                  f32_to_bf16(v[2]) | (uint32_t(f32_to_bf16(v[3])) << 16)};
-    } else {
-      *reinterpret_cast<f32x4_t*>(p) = v;
-    }
-    return;
-  }
-#pragma unroll
-  for (int u = 0; u < 4; ++u)
-    if (u < n) p[u] = Act<T>::from_f32(v[u]);
+// ---------------------------------------------------------------------------
+// What the tiles' epilogues share.  A wave has FN x FM accumulator tiles, FN of
+// columns; the matrix instruction leaves four columns of row (lane & 15) of each
+// with a lane, group g = lane / 16.  The weight rows are laid into LDS in an order
+// that gives a lane V consecutive columns, as many as fill a 16-byte store (16
+// hidden bytes, 8 bf16, 4 fp32; at most its 4 FN), and the four groups of a row
+// the V after each other: no exchange, and a store covers whole runs of a row.
+// Column of the wave's: tile j, group g, element u.
+// ---------------------------------------------------------------------------
+template <int V>
+__device__ __forceinline__ constexpr int tile_column(int j, int g) {
+  return j / (V / 4) * (4 * V) + V * g + 4 * (j % (V / 4));
 }
-
-// ---------------------------------------------------------------------------
-// What the tiles' epilogues share.  A wave has JT x IT accumulator tiles, tile j
-// of columns and i of rows; the lane holds columns c .. c + 3 of row (lane & 15),
-// c = (first column of tile j) + 4 (lane / 16).
-// ---------------------------------------------------------------------------
+// The tile's column that weight row r of its LDS rows holds.
+template <int FN, int V>
+__device__ __forceinline__ int weight_column(int r) {
+  constexpr int WN = 16 * FN;
+  const int t = r & (WN - 1);
+  return r - t + tile_column<V>(t >> 4, (t >> 2) & 3) + (t & 3);
+}
+// V of an epilogue: hidden rows take 4 FN columns together, others 16 bytes.
+template <int KIND, typename T, int FN>
+__device__ __host__ constexpr int run_columns() {
+  constexpr int most = KIND == kUp ? 16 : 16 / static_cast<int>(sizeof(T));
+  return 4 * FN < most ? 4 * FN : most;
+}
 
 // The activation of an accumulator tile in place (gated: the two hidden values
 // in v[0], v[1]), zeros in hidden columns past the width (their weight rows are
@@ -179,38 +181,103 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t t) {
   return max(t, static_cast<uint32_t>(__shfl_xor(static_cast<int>(t), 32, kWave)));
 }
 
-// Quantised hidden values of a tile into their row, from hidden column c (gated:
-// c / 2) on.
-template <int ACT>
-__device__ __forceinline__ void store_hidden4(uint8_t* row, int c, f32x4_t v, float inv) {
-  if constexpr (ACT == kActSwiglu)
-    *reinterpret_cast<uint16_t*>(row + c / 2) =
-        static_cast<uint16_t>(q8_pack4(v[0] * inv, v[1] * inv, 0.0f, 0.0f));
-  else
-    *reinterpret_cast<uint32_t*>(row + c) =
-        q8_pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-}
-
-template <typename T>
-__device__ __forceinline__ void store_out4(const QArgs& a, T* row, int c, f32x4_t v, bool vec) {
-  if (a.bias != nullptr) {
+// The hidden values of a row's accumulator tiles (columns c .. c + 4 FN - 1), their
+// largest finite magnitude in the lane.
+template <int ACT, int FN>
+__device__ __forceinline__ uint32_t hidden_row(f32x4_t* const (&v)[FN], int c, int Nout,
+                                               bool whole) {
+  uint32_t top = 0;
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (c + u < a.Nout) v[u] += a.bias[c + u];
+  for (int j = 0; j < FN; ++j) top = max(top, hidden4<ACT>(*v[j], c + 4 * j, Nout, whole));
+  if (__builtin_expect(__any(top >= kInfBits), 0)) {
+    top = 0;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) top = max(top, hidden_finite4<ACT>(*v[j]));
   }
-  store4(row + c, v, a.Nout - c, vec && c + 4 <= a.Nout);
+  return quad_max(top);
 }
 
-// Tile `local` of a group of mt x nt tiles: bands of eight row tiles, in a band the
-// column tiles in turn, each with all of the band's rows.  The 32 CUs of an XCD,
-// on consecutive tiles, then share eight row and four column tiles in its L2
-// (without bands, and 64 row tiles, each CU had rows of its own).
+// Them quantised, into hidden columns c .. (gated: c / 2 ..) of their row.
+template <int ACT, int FN>
+__device__ __forceinline__ void store_hidden(uint8_t* row, int c, f32x4_t* const (&v)[FN],
+                                             float inv) {
+  constexpr int ND = ACT == kActSwiglu ? FN / 2 : FN;  // dwords
+  uint32_t d[ND];
+#pragma unroll
+  for (int j = 0; j < ND; ++j) {
+    if constexpr (ACT == kActSwiglu) {
+      const f32x4_t &x = *v[2 * j], &y = *v[2 * j + 1];
+      d[j] = q8_pack4(x[0] * inv, x[1] * inv, y[0] * inv, y[1] * inv);
+    } else {
+      const f32x4_t& x = *v[j];
+      d[j] = q8_pack4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+    }
+  }
+  uint8_t* const p = row + (ACT == kActSwiglu ? c / 2 : c);
+  if constexpr (ND == 4) *reinterpret_cast<u32x4_t*>(p) = u32x4_t{d[0], d[1], d[2], d[3]};
+  else if constexpr (ND == 2) *reinterpret_cast<u32x2_t*>(p) = u32x2_t{d[0], d[1]};
+  else *reinterpret_cast<uint32_t*>(p) = d[0];
+}
+
+// The bias of a lane's columns (zeros without one, and past the last); c: the
+// wave's first column.
+template <int FN, int V>
+__device__ __forceinline__ void load_bias(const QArgs& a, int c, int g, f32x4_t (&b)[FN]) {
+#pragma unroll
+  for (int j = 0; j < FN; ++j)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int n = c + tile_column<V>(j, g) + u;
+      b[j][u] = a.bias != nullptr && n < a.Nout ? a.bias[n] : 0.0f;
+    }
+}
+
+// A lane's columns of an output row; vec: rows are 16-byte aligned.
+template <typename T, int FN, int V>
+__device__ __forceinline__ void store_out(const QArgs& a, T* row, int c, int g,
+                                          const f32x4_t* const (&v)[FN], const f32x4_t (&b)[FN],
+                                          bool vec) {
+  f32x4_t x[FN];
+#pragma unroll
+  for (int j = 0; j < FN; ++j) x[j] = *v[j] + b[j];
+  if (vec && c + 16 * FN <= a.Nout) {
+#pragma unroll
+    for (int j = 0; j < FN; j += V / 4) {
+      T* const p = row + c + tile_column<V>(j, g);
+      if constexpr (sizeof(T) == 2)
+        *reinterpret_cast<u32x4_t*>(p) =
+            u32x4_t{pack2_bf16(x[j][0], x[j][1]), pack2_bf16(x[j][2], x[j][3]),
+                    pack2_bf16(x[j + 1][0], x[j + 1][1]), pack2_bf16(x[j + 1][2], x[j + 1][3])};
+      else
+        *reinterpret_cast<f32x4_t*>(p) = x[j];
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < FN; ++j)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int n = c + tile_column<V>(j, g) + u;
+      if (n < a.Nout) row[n] = Act<T>::from_f32(x[j][u]);
+    }
+}
+
+// The four (or two) waves' largest magnitudes of a row.
+typedef __attribute__((ext_vector_type(4))) unsigned int top4_t;
+
+// Tile `local` of a group of mt x nt tiles: bands of at most eight row tiles, equal
+// ones, in a band the column tiles in turn, each with all of the band's rows.  The
+// 32 CUs of an XCD, on consecutive tiles, then share some eight row and four column
+// tiles in its L2 (without bands, and 64 row tiles, each CU had rows of its own).
 __device__ __forceinline__ void band_order(int local, int mt, int nt, int& m, int& n) {
-  const int band = local / (8 * nt);
-  const int in = local - band * 8 * nt;
-  const int h = min(8, mt - band * 8);
-  n = in / h;
-  m = band * 8 + in - n * h;
+  const int nb = (mt + 7) / 8, h = mt / nb, tall = mt - nb * h;  // `tall` bands of h + 1, then h
+  const int at = local / nt, edge = tall * (h + 1);
+  const bool in_tall = at < edge;
+  const int hb = in_tall ? h + 1 : h;
+  const int first = in_tall ? at / (h + 1) * (h + 1) : edge + (at - edge) / h * h;
+  const int in = local - first * nt;
+  n = in / hb;
+  m = first + in - n * hb;
 }
 
 // Source and destination row of row r of a tile (`rows` rows from r0 on).
@@ -296,11 +363,11 @@ __device__ __forceinline__ void mfma_q8(const Piece<true>& w, const Piece<true>&
 template <int KIND, int ACT, typename T, bool EXACT>
 __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
   constexpr bool kGated = ACT == kActSwiglu;
-  constexpr int FM = 4, FN = 4;
+  constexpr int FM = 4, FN = 4, V = run_columns<KIND, T, FN>();
   __shared__ __attribute__((aligned(16))) uint8_t lds[kMidStages * kMidStage];
   __shared__ __attribute__((aligned(16))) uint8_t s_sc[2][kMidScales];
   __shared__ int s_src[kMidTM], s_dst[kMidTM];
-  __shared__ uint32_t s_top[KIND == kUp ? 4 : 1][kMidTM];
+  __shared__ __attribute__((aligned(16))) uint32_t s_top[KIND == kUp ? kMidTM : 1][4];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -360,7 +427,8 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
     const uint8_t* const W = (routed ? a.W : a.Wsh) + g * a.Nout * a.pitch;
 #pragma unroll
     for (int u = 0; u < kMidLoadsW; ++u) {
-      const int n = min(t.n0 + 8 * (wv + kMidWaves * u) + (lane >> 3), a.Nout - 1);
+      const int n =
+          min(t.n0 + weight_column<FN, V>(8 * (wv + kMidWaves * u) + (lane >> 3)), a.Nout - 1);
       gw[u] = W + int64_t(n) * a.pitch + chunk * 16;
     }
     // scales: waves 0 and 1 the rows', two lanes of wave 2 the weight blocks'
@@ -493,48 +561,43 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
       start(nxt, nsrc, ndst);
       begin();
     }
-    const int c0 = cur.n0 + wn * 64 + 4 * (lane >> 4);
+    const int cw = cur.n0 + wn * 64, c0 = cw + 16 * (lane >> 4);
     if constexpr (KIND == kUp) {
       const bool whole = cur.n0 + kMidTN <= a.Nout;
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
-        uint32_t top = 0;
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-          top = max(top, hidden4<ACT>(acc[j][i], c0 + 16 * j, a.Nout, whole));
-        if (__builtin_expect(__any(top >= kInfBits), 0)) {
-          top = 0;
-#pragma unroll
-          for (int j = 0; j < FN; ++j) top = max(top, hidden_finite4<ACT>(acc[j][i]));
-        }
-        top = quad_max(top);
-        if (lane < 16) s_top[wn][wm * 64 + i * 16 + lane] = top;
+        f32x4_t* const v[FN] = {&acc[0][i], &acc[1][i], &acc[2][i], &acc[3][i]};
+        const uint32_t top = hidden_row<ACT, FN>(v, c0, a.Nout, whole);
+        if (lane < 16) s_top[wm * 64 + i * 16 + lane][wn] = top;
       }
       __syncthreads();
-      const int blk = (kGated ? cur.n0 / 2 : cur.n0) / kBlk + (kGated ? 0 : wn >> 1);
+      static_assert(kGated, "ungated up projections take the other tiles");
+      const int blk = cur.n0 / 2 / kBlk;
+      top4_t tops[FM];
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+        tops[i] = *reinterpret_cast<const top4_t*>(s_top[wm * 64 + i * 16 + (lane & 15)]);
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
-        if (drow[i] < 0 || blk * kBlk >= a.qpitch) continue;
-        const int row = wm * 64 + i * 16 + (lane & 15);
-        uint32_t top = max(s_top[wn & (kGated ? 0 : 2)][row], s_top[(wn & (kGated ? 0 : 2)) + 1][row]);
-        if (kGated) top = max(top, max(s_top[2][row], s_top[3][row]));
-        const int byte = q8_scale_byte(top);
-        const float inv = q8_inv(byte);
-        if ((wn & (kGated ? 3 : 1)) == 0 && lane < 16)
+        const int byte =
+            q8_scale_byte(max(max(tops[i][0], tops[i][1]), max(tops[i][2], tops[i][3])));
+        if (drow[i] < 0) continue;
+        f32x4_t* const v[FN] = {&acc[0][i], &acc[1][i], &acc[2][i], &acc[3][i]};
+        store_hidden<ACT, FN>(a.q + int64_t(drow[i]) * a.qpitch, c0, v, q8_inv(byte));
+        if (wn == 0 && lane < 16)
           a.s[int64_t(drow[i]) * a.qspitch + blk] = static_cast<uint8_t>(byte);
-        uint8_t* const qrow = a.q + int64_t(drow[i]) * a.qpitch;
-#pragma unroll
-        for (int j = 0; j < FN; ++j) store_hidden4<ACT>(qrow, c0 + 16 * j, acc[j][i], inv);
       }
     } else {
       T* const og = static_cast<T*>(KIND == kDense || cur.e < a.E ? a.dst : a.dst_sh);
-      const bool vec = (reinterpret_cast<uintptr_t>(og) & 15u) == 0 && a.ldo % 4 == 0;
+      const bool vec =
+          (reinterpret_cast<uintptr_t>(og) & 15u) == 0 && a.ldo * sizeof(T) % 16 == 0;
+      f32x4_t bias[FN];
+      load_bias<FN, V>(a, cw, lane >> 4, bias);
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
         if (drow[i] < 0) continue;
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-          store_out4(a, og + int64_t(drow[i]) * a.ldo, c0 + 16 * j, acc[j][i], vec);
+        const f32x4_t* const v[FN] = {&acc[0][i], &acc[1][i], &acc[2][i], &acc[3][i]};
+        store_out<T, FN, V>(a, og + int64_t(drow[i]) * a.ldo, cw, lane >> 4, v, bias, vec);
       }
     }
     if (!has_next) break;
@@ -558,7 +621,6 @@ template <int TM, bool GATED> struct Duo {
   static constexpr int kStages = TM == 128 ? 2 : 3;
   static constexpr int kTileX = TM * kBlk, kStage = (TM + TN) * kBlk;
   static constexpr int kLoadsX = TM / 8 / kWaves, kLoadsW = TN / 8 / kWaves;
-  static constexpr int kLoads = kLoadsX + kLoadsW;
   static constexpr int kScales = (TM + TN / kBlk) * 16;
   static constexpr int kBlocks = GATED ? 1 : 2;
   static constexpr int kWavesM = TM / 64, kWavesN = kWaves / kWavesM;
@@ -570,11 +632,11 @@ __global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qg
     QArgs a) {
   constexpr bool kGated = ACT == kActSwiglu;
   typedef Duo<TM, kGated> D;
-  constexpr int FM = D::FM, FN = D::FN, WN = FN * 16;
+  constexpr int FM = D::FM, FN = D::FN, WN = FN * 16, V = run_columns<KIND, T, FN>();
   __shared__ __attribute__((aligned(16))) uint8_t lds[D::kStages * D::kStage];
   __shared__ __attribute__((aligned(16))) uint8_t s_sc[2][D::kScales];
   __shared__ int s_src[TM], s_dst[TM];
-  __shared__ uint32_t s_top[KIND == kUp ? D::kWavesN : 1][TM];
+  __shared__ __attribute__((aligned(16))) uint32_t s_top[KIND == kUp ? TM : 1][D::kWavesN];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -619,7 +681,9 @@ __global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qg
     const uint8_t *gx[D::kLoadsX], *gw[D::kLoadsW], *gs;
 #pragma unroll
     for (int u = 0; u < D::kLoadsW; ++u)
-      gw[u] = W + int64_t(min(n0 + 8 * (wv + D::kWaves * u) + (lane >> 3), a.Nout - 1)) * a.pitch +
+      gw[u] = W +
+              int64_t(min(n0 + weight_column<FN, V>(8 * (wv + D::kWaves * u) + (lane >> 3)),
+                          a.Nout - 1)) * a.pitch +
               chunk * 16;
     auto issue_w = [&](int kt, int st) __attribute__((always_inline)) {
 #pragma unroll
@@ -627,9 +691,10 @@ __global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qg
         dma16(reinterpret_cast<const uint16_t*>(gw[u] + int64_t(kt) * kBlk),
               lds0 + st * D::kStage + D::kTileX + u * D::kWaves * 1024);
     };
-    auto issue_x = [&](int kt, int st) __attribute__((always_inline)) {
+    // nx: of the loads' 32-row groups, those that the tile has rows in
+    auto issue_x = [&](int kt, int st, auto nx) __attribute__((always_inline)) {
 #pragma unroll
-      for (int u = 0; u < D::kLoadsX; ++u)
+      for (int u = 0; u < decltype(nx)::value; ++u)
         dma16(reinterpret_cast<const uint16_t*>(gx[u] + int64_t(kt) * kBlk),
               lds0 + st * D::kStage + u * D::kWaves * 1024);
     };
@@ -655,11 +720,6 @@ __global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qg
     gs = wv < TM / 64 ? a.Xs + int64_t(s_src[(64 * wv + lane) & (TM - 1)]) * a.spitch
                       : Ws + int64_t(min(n0 / kBlk + (lane & 1), nbw - 1)) * a.spitch;
     issue_scales(0);
-    issue_x(0, 0);
-    if (D::kStages > 2 && KT > 1) {
-      issue_w(1, 1);
-      issue_x(1, 1);
-    }
 
     f32x4_t acc[FN][FM];
 #pragma unroll
@@ -669,16 +729,22 @@ __global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qg
     // the k-loop for a wave with NI 16-row tiles
     auto run = [&](auto ni_c) __attribute__((always_inline)) {
       constexpr int NI = decltype(ni_c)::value;
+      typedef std::integral_constant<int, (TM == 64 && NI > 0 && NI <= 2 ? 1 : D::kLoadsX)> NX;
+      issue_x(0, 0, NX{});
+      if (D::kStages > 2 && KT > 1) {
+        issue_w(1, 1);
+        issue_x(1, 1, NX{});
+      }
       int st = 0;
       for (int kt = 0; kt < KT; ++kt) {
-        if (D::kStages > 2 && kt + 1 < KT) slot_wait<D::kLoads>();
+        if (D::kStages > 2 && kt + 1 < KT) slot_wait<D::kLoadsW + NX::value>();
         else slot_wait<0>();
         slot_barrier();
         constexpr int kAhead = D::kStages - 1;
         if (kt + kAhead < KT) {
           const int to = st + kAhead >= D::kStages ? st + kAhead - D::kStages : st + kAhead;
           issue_w(kt + kAhead, to);
-          issue_x(kt + kAhead, to);
+          issue_x(kt + kAhead, to, NX{});
           if ((kt & 15) == 0 && kt + 16 < KT) issue_scales((kt >> 4) + 1);
         }
         if constexpr (NI > 0) {
@@ -720,23 +786,17 @@ __global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qg
         for (int i = 0; i < FM; ++i) asm volatile("" : "+v"(acc[j][i]));
     }
 
-    const int c0 = n0 + wn * WN + 4 * (lane >> 4);
+    const int cw = n0 + wn * WN, c0 = cw + 4 * FN * (lane >> 4);
     if constexpr (KIND == kUp) {
       const bool whole = n0 + D::TN <= a.Nout;
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
         if (TM == 64 && i * 16 >= rows) continue;
-        uint32_t top = 0;
+        f32x4_t* v[FN];
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
-          top = max(top, hidden4<ACT>(acc[j][i], c0 + 16 * j, a.Nout, whole));
-        if (__builtin_expect(__any(top >= kInfBits), 0)) {
-          top = 0;
-#pragma unroll
-          for (int j = 0; j < FN; ++j) top = max(top, hidden_finite4<ACT>(acc[j][i]));
-        }
-        top = quad_max(top);
-        if (lane < 16) s_top[wn][wm * 64 + i * 16 + lane] = top;
+        for (int j = 0; j < FN; ++j) v[j] = &acc[j][i];
+        const uint32_t top = hidden_row<ACT, FN>(v, c0, a.Nout, whole);
+        if (lane < 16) s_top[wm * 64 + i * 16 + lane][wn] = top;
       }
       __syncthreads();
       const int blk = (kGated ? n0 / 2 : n0) / kBlk;
@@ -744,27 +804,31 @@ __global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qg
       for (int i = 0; i < FM; ++i) {
         const int row = wm * 64 + i * 16 + (lane & 15);
         const int64_t drow = s_dst[row];
-        if (drow < 0) continue;
-        uint32_t top = s_top[0][row];
+        uint32_t top = s_top[row][0];
 #pragma unroll
-        for (int w = 1; w < D::kWavesN; ++w) top = max(top, s_top[w][row]);
+        for (int w = 1; w < D::kWavesN; ++w) top = max(top, s_top[row][w]);
         const int byte = q8_scale_byte(top);
-        const float inv = q8_inv(byte);
-        if (wn == 0 && lane < 16) a.s[drow * a.qspitch + blk] = static_cast<uint8_t>(byte);
+        if (drow < 0) continue;
+        f32x4_t* v[FN];
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
-          store_hidden4<ACT>(a.q + drow * a.qpitch, c0 + 16 * j, acc[j][i], inv);
+        for (int j = 0; j < FN; ++j) v[j] = &acc[j][i];
+        store_hidden<ACT, FN>(a.q + drow * a.qpitch, c0, v, q8_inv(byte));
+        if (wn == 0 && lane < 16) a.s[drow * a.qspitch + blk] = static_cast<uint8_t>(byte);
       }
     } else {
       T* const og = static_cast<T*>(routed ? a.dst : a.dst_sh);
-      const bool vec = (reinterpret_cast<uintptr_t>(og) & 15u) == 0 && a.ldo % 4 == 0;
+      const bool vec =
+          (reinterpret_cast<uintptr_t>(og) & 15u) == 0 && a.ldo * sizeof(T) % 16 == 0;
+      f32x4_t bias[FN];
+      load_bias<FN, V>(a, cw, lane >> 4, bias);
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
         const int64_t drow = s_dst[wm * 64 + i * 16 + (lane & 15)];
         if (drow < 0) continue;
+        const f32x4_t* v[FN];
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
-          store_out4(a, og + drow * a.ldo, c0 + 16 * j, acc[j][i], vec);
+        for (int j = 0; j < FN; ++j) v[j] = &acc[j][i];
+        store_out<T, FN, V>(a, og + drow * a.ldo, cw, lane >> 4, v, bias, vec);
       }
     }
     __syncthreads();
@@ -801,6 +865,17 @@ constexpr int kTallBuf = 4 * kTallHalf;  // X0 X1 W0 W1
 constexpr int kTallMinKT = 4;            // k-tiles
 constexpr int kTallScales = (kTallTM + 2) * 16;
 
+// The column, of the tile's, that row r of region h of the weights holds.  A wave
+// has rows 32 wn .. of either region, two 16-column tiles in each.  wide: the
+// tile has columns past 128, and a wave 64 consecutive ones; else the first region
+// has them all, and a wave 32.
+template <int KIND, typename T>
+__device__ __forceinline__ int tall_column(int r, int h, bool wide) {
+  const int wn = r >> 5, j = (r >> 4) & 1, g = (r >> 2) & 3, u = r & 3;
+  return wide ? 64 * wn + tile_column<run_columns<KIND, T, 4>()>(2 * h + j, g) + u
+              : 32 * wn + tile_column<run_columns<KIND, T, 2>()>(j, g) + u;
+}
+
 template <int KIND, int ACT, typename T>
 __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
   constexpr bool kGated = ACT == kActSwiglu;
@@ -810,7 +885,7 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t s_sc[3 * kTallScales];
   __shared__ int s_list[2][kTallTM];
   __shared__ int s_toff[128];
-  __shared__ uint32_t s_top[KIND == kUp ? 2 : 1][4][kTallTM];
+  __shared__ __attribute__((aligned(16))) uint32_t s_top[KIND == kUp ? kTallTM : 1][4];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -862,6 +937,10 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
     return t;
   };
 
+  // gated tiles are always wide: they fill whole blocks of the hidden rows
+  auto wide = [&](const TTile& t) __attribute__((always_inline)) {
+    return kGated || t.n0 + 128 < a.Nout;
+  };
   // the load stream's tile: byte offsets of this lane's rows, and of its scales'
   uint32_t va[4], vw[4];
   const uint8_t* wbase = a.W;
@@ -879,7 +958,7 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
     for (int q = 0; q < 4; ++q) {
       const int r = 128 * (q >> 1) + 8 * (wv + kTallWaves * (q & 1)) + (lane >> 3);
       va[q] = static_cast<uint32_t>(source(t, lb, r)) * static_cast<uint32_t>(a.pitch) + chunk * 16;
-      const int n = min(r, a.Nout - 1 - t.n0);
+      const int n = min(tall_column<KIND, T>(r & 127, q >> 1, wide(t)), a.Nout - 1 - t.n0);
       vw[q] = static_cast<uint32_t>(n) * static_cast<uint32_t>(a.pitch) + chunk * 16;
     }
     const bool routed = !kTable || t.e < a.E;
@@ -930,7 +1009,7 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
   const uint32_t sl = (lane & 15) * 16 + wm * 256;
 
   i32x8_t fx[4], fa[2], fb[2];
-  int sx[4], sw0, sw1;
+  int sx[4], sw;
   auto read_x = [&](int b, int h, int n) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -990,11 +1069,11 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) acc[j][i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     // one instantiation per tile height (NX = 0, 2 or 4 16-row tiles per wave in
-    // the second half), with or without columns past 128 (CA)
+    // the second half), with or without columns past 128 (CA: wide)
     auto run = [&](auto nx_c, auto ca_c) __attribute__((always_inline)) {
       constexpr int NX = decltype(nx_c)::value;
       constexpr bool CA = decltype(ca_c)::value;
-      auto mfma_q = [&](int h, int c, const i32x8_t (&f)[2], int sw) __attribute__((always_inline)) {
+      auto mfma_q = [&](int h, int c, const i32x8_t (&f)[2]) __attribute__((always_inline)) {
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int j = 0; j < 2; ++j)
@@ -1017,17 +1096,16 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
         // phase 0: X0 x W0
         read_x(b, 0, 4);
         read_sx(so, 0, 4);
-        sw0 = s_sc[so + kTallTM * 16];
-        sw1 = s_sc[so + kTallTM * 16 + 16];
+        sw = s_sc[so + kTallTM * 16 + (CA ? (wn >> 1) * 16 : 0)];
         issue_w(lt, b, 0);
         settle();
-        mfma_q(0, 0, p, sw0);
+        mfma_q(0, 0, p);
         slot_barrier();
         // phase 1: X0 x W1
         if (CA) read_w(q, b, 1);
         issue_x(lt, b, 0, nx);
         settle();
-        if (CA) mfma_q(0, 1, q, sw1);
+        if (CA) mfma_q(0, 1, q);
         slot_barrier();
         // phase 2: X1 x W1
         if (NX > 0) {
@@ -1036,13 +1114,13 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
         }
         issue_w(lt, b, 1);
         settle();
-        if (CA && NX > 0) mfma_q(1, 1, q, sw1);
+        if (CA && NX > 0) mfma_q(1, 1, q);
         slot_barrier();
         // phase 3: X1 x W0, and the next k-tile's W0
         read_w(q, b ^ 1, 0);
         issue_x(lt, b, 1, nx);
         settle();
-        if (NX > 0) mfma_q(1, 0, p, sw0);
+        if (NX > 0) mfma_q(1, 0, p);
         slot_barrier();
       };
       // No branches inside a k-tile: tables and scales are asked for between them,
@@ -1087,7 +1165,7 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(acc[j][i]));
     };
-    if (cur.n0 + 128 < a.Nout) {
+    if (wide(cur)) {
       if (cur.rows > 192) run(std::integral_constant<int, 4>{}, std::true_type{});
       else if (cur.rows > 128) run(std::integral_constant<int, 2>{}, std::true_type{});
       else run(std::integral_constant<int, 0>{}, std::true_type{});
@@ -1097,108 +1175,66 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
       else run(std::integral_constant<int, 0>{}, std::false_type{});
     }
 
-    // epilogue: tile 2 c + j of columns starts at n0 + 128 c + 32 wn + 16 j, tile i
-    // of rows at 128 (i / 4) + 16 (2 (i % 4) + wm).  Lanes l and l ^ 16 exchange
-    // runs of a wave's two adjacent column tiles, so that a store writes 8
-    // consecutive columns (hidden: 8 bytes, gated 4).
+    // epilogue: tile i of rows starts at 128 (i / 4) + 16 (2 (i % 4) + wm); the
+    // wave has 64 columns, or 32 (tall_column)
     const int lane = fresh_lane();
-    const int g = lane >> 4, odd = g & 1;
-    if constexpr (KIND == kUp) {
-      const bool whole = cur.n0 + kTallTN <= a.Nout;
+    const int g = lane >> 4;
+    auto finish = [&](auto fn_c) __attribute__((always_inline)) {
+      constexpr int FN = decltype(fn_c)::value;
+      constexpr int V = run_columns<KIND, T, FN>();
+      const int cw = cur.n0 + 16 * FN * wn, c0 = cw + 4 * FN * g;
+      if constexpr (KIND == kUp) {
+        const bool whole = cur.n0 + 64 * FN <= a.Nout;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int row = 128 * (i >> 2) + 16 * (2 * (i & 3) + wm) + (lane & 15);
-        uint32_t top[2];
+        for (int i = 0; i < 8; ++i) {
+          f32x4_t* v[FN];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int c0 = cur.n0 + 128 * c + 32 * wn + 4 * g;
-          top[c] = max(hidden4<ACT>(acc[2 * c][i], c0, a.Nout, whole),
-                       hidden4<ACT>(acc[2 * c + 1][i], c0 + 16, a.Nout, whole));
-          if (__builtin_expect(__any(top[c] >= kInfBits), 0))
-            top[c] = max(hidden_finite4<ACT>(acc[2 * c][i]), hidden_finite4<ACT>(acc[2 * c + 1][i]));
+          for (int j = 0; j < FN; ++j) v[j] = &acc[j][i];
+          const uint32_t top = hidden_row<ACT, FN>(v, c0, a.Nout, whole);
+          if (lane < 16) s_top[128 * (i >> 2) + 16 * (2 * (i & 3) + wm) + lane][wn] = top;
         }
-        if (kGated) top[0] = max(top[0], top[1]);
+        slot_wait<15>();
+        slot_barrier();
+        // a block of 128 hidden columns lies with two waves, or four (gated, not wide)
+        constexpr bool kPair = FN == 4 && !kGated;
+        const int blk = kGated ? cur.n0 / 2 / kBlk : cur.n0 / kBlk + (kPair ? wn >> 1 : 0);
 #pragma unroll
-        for (int c = 0; c < (kGated ? 1 : 2); ++c) {
-          top[c] = quad_max(top[c]);
-          if (lane < 16) s_top[c][wn][row] = top[c];
-        }
-      }
-      slot_wait<15>();
-      slot_barrier();
+        for (int i = 0; i < 8; ++i) {
+          const int row = 128 * (i >> 2) + 16 * (2 * (i & 3) + wm) + (lane & 15);
+          const top4_t t = *reinterpret_cast<const top4_t*>(s_top[row]);
+          const uint32_t t01 = max(t[0], t[1]), t23 = max(t[2], t[3]);
+          const int byte = q8_scale_byte(kPair ? (wn < 2 ? t01 : t23) : max(t01, t23));
+          const int64_t drow = cur.r0 + row;
+          f32x4_t* v[FN];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int row = 128 * (i >> 2) + 16 * (2 * (i & 3) + wm) + (lane & 15);
-        if (row >= cur.rows) continue;
-        const int64_t drow = cur.r0 + row;
-        uint8_t* const qrow = a.q + drow * a.qpitch;
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int blk = kGated ? cur.n0 / 2 / kBlk : cur.n0 / kBlk + c;
-          if (blk * kBlk >= a.qpitch) continue;
-          const int tc = kGated ? 0 : c;
-          const int byte = q8_scale_byte(max(max(s_top[tc][0][row], s_top[tc][1][row]),
-                                             max(s_top[tc][2][row], s_top[tc][3][row])));
-          const float inv = q8_inv(byte);
-          if (wn == 0 && lane < 16 && (!kGated || c == 0))
-            a.s[drow * a.qspitch + blk] = static_cast<uint8_t>(byte);
-          const f32x4_t &v0 = acc[2 * c][i], &v1 = acc[2 * c + 1][i];
-          const int cw = cur.n0 + 128 * c + 32 * wn;
-          if constexpr (kGated) {
-            const uint32_t p0 = q8_pack4(v0[0] * inv, v0[1] * inv, 0.0f, 0.0f) & 0xffffu;
-            const uint32_t p1 = q8_pack4(v1[0] * inv, v1[1] * inv, 0.0f, 0.0f) & 0xffffu;
-            const uint32_t r = __shfl_xor(odd ? p0 : p1, 16, kWave);
-            *reinterpret_cast<uint32_t*>(qrow + cw / 2 + 8 * odd + 2 * (g - odd)) =
-                odd ? (r | (p1 << 16)) : (p0 | (r << 16));
-          } else {
-            const uint32_t p0 = q8_pack4(v0[0] * inv, v0[1] * inv, v0[2] * inv, v0[3] * inv);
-            const uint32_t p1 = q8_pack4(v1[0] * inv, v1[1] * inv, v1[2] * inv, v1[3] * inv);
-            const uint32_t r = __shfl_xor(odd ? p0 : p1, 16, kWave);
-            *reinterpret_cast<u32x2_t*>(qrow + cw + 16 * odd + 4 * (g - odd)) =
-                odd ? u32x2_t{r, p1} : u32x2_t{p0, r};
+          for (int j = 0; j < FN; ++j) v[j] = &acc[j][i];
+          if (row < cur.rows && blk * kBlk < a.qpitch) {
+            store_hidden<ACT, FN>(a.q + drow * a.qpitch, c0, v, q8_inv(byte));
+            if ((wn & (kPair ? 1 : 3)) == 0 && lane < 16)
+              a.s[drow * a.qspitch + blk] = static_cast<uint8_t>(byte);
           }
         }
-      }
-    } else {
-      T* const og = static_cast<T*>(!kTable || cur.e < a.E ? a.dst : a.dst_sh);
-      const bool vec = (reinterpret_cast<uintptr_t>(og) & 15u) == 0 && a.ldo % 8 == 0;
+      } else {
+        T* const og = static_cast<T*>(!kTable || cur.e < a.E ? a.dst : a.dst_sh);
+        const bool vec =
+            (reinterpret_cast<uintptr_t>(og) & 15u) == 0 && a.ldo * sizeof(T) % 16 == 0;
+        f32x4_t bias[FN];
+        load_bias<FN, V>(a, cw, g, bias);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int row = 128 * (i >> 2) + 16 * (2 * (i & 3) + wm) + (lane & 15);
-        if (row >= cur.rows) continue;
-        int64_t drow = cur.r0 + row;
-        if (KIND == kDown) drow = cur.e < a.E ? s_list[lb][row] : drow - a.off[a.E];
-        T* const orow = og + drow * a.ldo;
+        for (int i = 0; i < 8; ++i) {
+          const int row = 128 * (i >> 2) + 16 * (2 * (i & 3) + wm) + (lane & 15);
+          if (row >= cur.rows) continue;
+          int64_t drow = cur.r0 + row;
+          if (KIND == kDown) drow = cur.e < a.E ? s_list[lb][row] : drow - a.off[a.E];
+          const f32x4_t* v[FN];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int cw = cur.n0 + 128 * c + 32 * wn;  // first column of the pair
-          if (cw >= a.Nout) continue;
-          f32x4_t v[2] = {acc[2 * c][i], acc[2 * c + 1][i]};
-          if (sizeof(T) == 2 && vec && cw + 32 <= a.Nout) {
-            if (KIND == kDense && a.bias != nullptr) {
-#pragma unroll
-              for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int u = 0; u < 4; ++u) v[j][u] += a.bias[cw + 16 * j + 4 * g + u];
-            }
-            u32x2_t pk[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-              pk[j] = u32x2_t{pack2_bf16(v[j][0], v[j][1]), pack2_bf16(v[j][2], v[j][3])};
-            const u32x2_t keep = odd ? pk[1] : pk[0];
-            const u32x2_t send = odd ? pk[0] : pk[1];
-            const uint32_t q0 = __shfl_xor(send[0], 16, kWave);
-            const uint32_t q1 = __shfl_xor(send[1], 16, kWave);
-            *reinterpret_cast<u32x4_t*>(orow + cw + 16 * odd + 4 * (g - odd)) =
-                odd ? u32x4_t{q0, q1, keep[0], keep[1]} : u32x4_t{keep[0], keep[1], q0, q1};
-          } else {
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-              store_out4(a, orow, cw + 16 * j + 4 * g, v[j], vec);
-          }
+          for (int j = 0; j < FN; ++j) v[j] = &acc[j][i];
+          store_out<T, FN, V>(a, og + drow * a.ldo, cw, g, v, bias, vec);
         }
       }
-    }
+    };
+    if (wide(cur)) finish(std::integral_constant<int, 4>{});
+    else finish(std::integral_constant<int, 2>{});
     if (!has_next) break;
     // the next tile's first piece of scales
     sc = sc == 2 ? 0 : sc + 1;
@@ -1267,7 +1303,8 @@ FfnPlan q8_plan(const Shape& s, StepKind kind, int64_t rows) {
   (void)kind;
   FfnPlan p;
   p.tm = p.tm_up = kMidTM;
-  p.tn_up = p.tn_down = kMidTN;
+  p.tn_up = kMidTN;
+  p.tn_down = s.bf16 ? kMidTN : 128;
   const bool many = rows / s.E >= 144, few = rows / s.E <= 48;
   p.tall_up = many && !exact_up(s) && tall_capable(s.tokens(), s.d);
   p.tall_down = many && s.bf16 && tall_capable(s.mid_rows(), s.d_ff);
@@ -1343,7 +1380,7 @@ hipError_t launch_q8_down(const Shape& s, const FfnPlan& plan, const QuantWeight
     return s.bf16 ? launch_duo<kDown, kActNone, uint16_t, true, 64>(a, st)
                   : launch_duo<kDown, kActNone, float, true, 64>(a, st);
   if (s.bf16) return launch<kDown, kActNone, uint16_t, false>(a, st);
-  return launch<kDown, kActNone, float, true>(a, st);
+  return launch_duo<kDown, kActNone, float, true, 128>(a, st);
 }
 
 hipError_t launch_q8_linear(const Q8& x, int64_t M, int K, const void* W, const void* Ws, int N,
