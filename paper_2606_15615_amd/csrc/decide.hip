@@ -127,6 +127,7 @@ struct ListArgs {
   int S, T;  // shared experts, tokens of the batch
   int tm_up, tm, nt_up, nt_down, tall_up, tall_down, cus;
   int in_list;  // the down projection leaves its rows in list order (row_dst = identity)
+  int half_up, half_down;  // columns of a tall tile may be halved: column tiles then, or 0
   int32_t *off, *tiles, *list, *pos, *row_dst;
 };
 
@@ -153,9 +154,18 @@ __device__ __forceinline__ int list_offsets(int t, int E, const ListArgs& a, boo
 __device__ __forceinline__ void tile_table(int t, int E, const ListArgs& a, bool down) {
   const int lane = threadIdx.x & (kWave - 1);
   const int G = E + a.S;
-  const int nt = down ? a.nt_down : a.nt_up;
+  int nt = down ? a.nt_down : a.nt_up;
   int tm = down ? a.tm : a.tm_up;
-  if (down ? a.tall_down : a.tall_up) tm = tall_rows(t, E, a.S, a.T, nt, a.cus);
+  const bool tall = (down ? a.tall_down : a.tall_up) != 0;
+  if (tall) tm = tall_rows(t, E, a.S, a.T, nt, a.cus);
+  // 8-bit tiles: half as wide where that still leaves one each for the CUs
+  const int half = down ? a.half_down : a.half_up;
+  bool halved = false;
+  if (tall && half != 0) {
+    const int mt = wave_sum_i32((t + tm - 1) / tm) + a.S * ((a.T + tm - 1) / tm);
+    halved = mt * half <= a.cus;
+    if (halved) nt = half;
+  }
   const int n = (t + tm - 1) / tm * nt;
   const int x = wave_incl_scan_i32(n);
   int32_t* const out = a.tiles + (down ? G + 1 : 0);
@@ -164,6 +174,7 @@ __device__ __forceinline__ void tile_table(int t, int E, const ListArgs& a, bool
     const int ns = (a.T + tm - 1) / tm * nt;
     for (int s2 = 0; s2 <= a.S; ++s2) out[E + s2] = x + s2 * ns;
     a.tiles[2 * (G + 1) + (down ? 1 : 0)] = tm;
+    a.tiles[2 * (G + 1) + 2 + (down ? 1 : 0)] = halved ? 1 : 0;
   }
 }
 
@@ -1163,7 +1174,8 @@ static ListArgs list_args(const Shape& s, const FfnPlan& plan, const Buffers& b)
                   (s.up_rows() + plan.tn_up - 1) / plan.tn_up,
                   (s.d + plan.tn_down - 1) / plan.tn_down * plan.split_down,
                   plan.tall_up ? 1 : 0, plan.tall_down ? 1 : 0, device_cus(), s.cache8 ? 1 : 0,
-                  b.off, b.tiles, b.list, b.pos, b.row_dst};
+                  plan.half_up ? (s.up_rows() + 127) / 128 : 0,
+                  plan.half_down ? (s.d + 127) / 128 : 0, b.off, b.tiles, b.list, b.pos, b.row_dst};
 }
 
 // Every wave ranks its branches by a ballot per expert, which the launch of its

@@ -97,7 +97,8 @@ struct Buffers {
   int32_t* stats_bs;// [B][4] recompute, unmatched, matched, sync per sample
   int32_t* rflags;  // router: one non-finite flag per block
   int32_t* tiles;   // [2][E+S+1] grouped-GEMM tile prefix per group (up, down), then the
-                    // rows of a tile, at most, of either (256 x 256 tiles)
+                    // rows of a tile, at most, of either (256 x 256 tiles), then whether
+                    // its columns are halved
   int32_t* row_dst; // [B*N*k] cache row of each listed branch: (f/k)*k + sigma(f)
   int32_t* wide;    // [B][kWideWords] per-sample scratch of the multi-block decision path
   void* mid;        // [B*N*k + S*T][d_ff] FFN activation of listed and shared rows
@@ -125,6 +126,7 @@ struct FfnPlan {
   bool wide_up = false;  // the up projection takes the expert-wide kernel
   int tm_up = 128;       // M tile of the up projection's tile table
   bool tall_up = false, tall_down = false;  // the 256 x 256 tiles (tm chosen on the device)
+  bool half_up = false, half_down = false;  // their columns too (8-bit experts)
 };
 constexpr int kThinSplit = 4;
 // A ratio-mode cache step takes the weight-streaming tiles for both projections
@@ -204,9 +206,10 @@ struct QuantWeights {
   const void *up = nullptr, *up_s = nullptr, *down = nullptr, *down_s = nullptr;
   const void *up_sh = nullptr, *up_sh_s = nullptr, *down_sh = nullptr, *down_sh_s = nullptr;
 };
+// mask: rows whose byte is 0 are left out (or null).
 hipError_t launch_quant_rows(const void* src, bool bf16, int64_t rows, int K, int64_t ld,
-                             const int32_t* slot, int64_t slots, uint8_t* q, uint8_t* s,
-                             float* norm, hipStream_t st);
+                             const int32_t* slot, const uint8_t* mask, int64_t slots, uint8_t* q,
+                             uint8_t* s, float* norm, hipStream_t st);
 hipError_t launch_dequant_rows(const uint8_t* q, const uint8_t* s, int64_t slots, int K,
                                const int32_t* slot, int64_t rows, void* dst, bool bf16,
                                int64_t ld, hipStream_t st);

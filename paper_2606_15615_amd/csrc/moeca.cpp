@@ -95,7 +95,7 @@ Layout make_layout(const Shape& s, bool external_mid = false, bool partials = tr
   b[R_CNT_BS] = size_t(s.B) * s.E * 4;
   b[R_STATS_BS] = size_t(s.B) * 4 * 4;
   b[R_RFLAGS] = size_t(moeca::router_blocks(s)) * 4;
-  b[R_TILES] = (size_t(2) * (s.groups() + 1) + 2) * 4;
+  b[R_TILES] = (size_t(2) * (s.groups() + 1) + 4) * 4;
   b[R_ROW_DST] = nbr * 4;
   b[R_ENT] = size_t(s.B) * s.E * ((size_t(s.N) + 15) / 16) * 2 * 8;
   b[R_CNT_CH] = size_t(s.B) * ((size_t(s.N) * s.k + 1023) / 1024) * s.E * 4;
@@ -203,8 +203,10 @@ hipError_t ffn_up(const moeca_layer* L, const Shape& s, const void* x, const moe
   const moeca::LaunchEvents ev = moeca::launch_events();
   moeca::launch_events() = {ev.start, nullptr};
   const moeca::Q8 q = moeca::q8_view(b.x8, s.tokens(), s.d);
+  // only the tokens that a routed expert reads, unless shared experts read all
   const hipError_t e = moeca::launch_quant_rows(x, s.bf16, s.tokens(), s.d, s.d, nullptr,
-                                                s.tokens(), q.q, q.s, nullptr, st);
+                                                s.S == 0 ? b.sync : nullptr, s.tokens(), q.q, q.s,
+                                                nullptr, st);
   if (e != hipSuccess) return e;
   moeca::launch_events() = {nullptr, ev.stop};
   return moeca::launch_q8_up(s, L->pol.act, plan, L->qw, b, st);

@@ -56,8 +56,10 @@ struct QArgs {
   const int32_t *off, *tile_off, *list, *row_dst;
   int E, G, k;     // routed groups, all groups, branches a token
   int M;           // dense: rows
-  const int32_t* tm;  // rows of a 256-column tile, at most (from the lists kernel)
-  int dense_tm;       // the same of a dense product
+  // of the 256-column tiles: rows, at most, and (tm[2]) whether they are 128
+  // columns wide (from the lists kernel; dense: from the host)
+  const int32_t* tm;
+  int dense_tm, dense_half;
   int pitch, spitch;
   int Nout;        // weight rows of a group
   int64_t ldo;     // elements of an output row (down, dense)
@@ -854,7 +856,9 @@ __global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qg
 // a little longer.
 //
 // The rows of a tile, 256, 192 or 128, come from the lists kernel's table (dense:
-// from the host) as for the bf16 kernel.
+// from the host) as for the bf16 kernel, and so do its columns: 128 where tiles of
+// 256 would leave half of the CUs without one (a cache step that recomputes few
+// branches, which the host cannot know).
 // ---------------------------------------------------------------------------
 constexpr int kTallTM = 256;
 constexpr int kTallTN = 256;
@@ -891,8 +895,10 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
   const int lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wv >> 2, wn = wv & 3;  // wm is also the ping-pong group
-  const int TM = kTable ? *a.tm : a.dense_tm;
-  const int nt = (a.Nout + kTallTN - 1) / kTallTN;
+  const int TM = kTable ? a.tm[0] : a.dense_tm;
+  const bool half = !kGated && (kTable ? a.tm[2] : a.dense_half) != 0;
+  const int TN = half ? 128 : kTallTN;
+  const int nt = (a.Nout + TN - 1) / TN;
   const int total = kTable ? a.tile_off[a.G] : (a.M + TM - 1) / TM * nt;
   const int per = (total + kXcds - 1) / kXcds;
   const int lo = (blockIdx.x % kXcds) * per;
@@ -933,13 +939,13 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
     band_order(__builtin_amdgcn_readfirstlane(L - e_base), mt, nt, m, n);
     t.r0 = __builtin_amdgcn_readfirstlane(o0 + static_cast<int>(int64_t(m) * cnt / mt));
     t.rows = __builtin_amdgcn_readfirstlane(o0 + static_cast<int>(int64_t(m + 1) * cnt / mt) - t.r0);
-    t.n0 = __builtin_amdgcn_readfirstlane(n * kTallTN);
+    t.n0 = __builtin_amdgcn_readfirstlane(n * TN);
     return t;
   };
 
   // gated tiles are always wide: they fill whole blocks of the hidden rows
   auto wide = [&](const TTile& t) __attribute__((always_inline)) {
-    return kGated || t.n0 + 128 < a.Nout;
+    return kGated || (!half && t.n0 + 128 < a.Nout);
   };
   // the load stream's tile: byte offsets of this lane's rows, and of its scales'
   uint32_t va[4], vw[4];
@@ -1270,7 +1276,9 @@ hipError_t launch_duo(const QArgs& a, hipStream_t st) {
 template <int ACT>
 hipError_t launch_up(const QArgs& a, bool exact, const FfnPlan& plan, hipStream_t st) {
   if (plan.tall_up) return launch_tall<kUp, ACT, float>(a, st);
-  if (plan.tm_up == 64) return launch_duo<kUp, ACT, float, true, 64>(a, st);
+  if (plan.tm_up == 64)
+    return exact ? launch_duo<kUp, ACT, float, true, 64>(a, st)
+                 : launch_duo<kUp, ACT, float, false, 64>(a, st);
   if constexpr (ACT == kActSwiglu)
     return exact ? launch<kUp, ACT, float, true>(a, st) : launch<kUp, ACT, float, false>(a, st);
   else
@@ -1302,20 +1310,23 @@ Q8 q8_view(void* base, int64_t rows, int64_t K) {
 FfnPlan q8_plan(const Shape& s, StepKind kind, int64_t rows) {
   (void)kind;
   FfnPlan p;
-  p.tm = p.tm_up = kMidTM;
-  p.tn_up = kMidTN;
+  p.tm = p.tm_up = 128;
+  const int64_t mean = rows / s.E;
+  const bool many = mean >= 144, few = mean <= 48, exact = exact_up(s);
+  p.tn_up = s.swiglu ? kMidTN : 128;
   p.tn_down = s.bf16 ? kMidTN : 128;
-  const bool many = rows / s.E >= 144, few = rows / s.E <= 48;
-  p.tall_up = many && !exact_up(s) && tall_capable(s.tokens(), s.d);
+  p.tall_up = many && !exact && tall_capable(s.tokens(), s.d);
   p.tall_down = many && s.bf16 && tall_capable(s.mid_rows(), s.d_ff);
-  if (p.tall_up) p.tm_up = kTallTM;
+  p.half_up = !s.swiglu;
+  p.half_down = true;
+  if (p.tall_up) {
+    p.tm_up = kTallTM;
+    p.tn_up = kTallTN;
+  }
   if (p.tall_down) p.tm = kTallTM;
   if (few) {
     p.tm_up = p.tm = 64;
     p.tn_down = 128;
-    if (!s.swiglu) p.tn_up = 128;
-  } else if (!s.swiglu && !p.tall_up) {
-    p.tn_up = 128;
   }
   return p;
 }
@@ -1377,7 +1388,7 @@ hipError_t launch_q8_down(const Shape& s, const FfnPlan& plan, const QuantWeight
   a.tm = b.tiles + 2 * (s.groups() + 1) + 1;
   if (plan.tall_down) return launch_tall<kDown, kActNone, uint16_t>(a, st);
   if (plan.tm == 64)
-    return s.bf16 ? launch_duo<kDown, kActNone, uint16_t, true, 64>(a, st)
+    return s.bf16 ? launch_duo<kDown, kActNone, uint16_t, false, 64>(a, st)
                   : launch_duo<kDown, kActNone, float, true, 64>(a, st);
   if (s.bf16) return launch<kDown, kActNone, uint16_t, false>(a, st);
   return launch_duo<kDown, kActNone, float, true, 128>(a, st);
@@ -1400,11 +1411,12 @@ hipError_t launch_q8_linear(const Q8& x, int64_t M, int K, const void* W, const 
   a.dst = out;
   if (bf16 && M >= 256 && tall_capable(M, K)) {
     a.dense_tm = tall_rows_one(M, (N + kTallTN - 1) / kTallTN, device_cus());
+    a.dense_half = 0;
     return launch_tall<kDense, kActNone, uint16_t>(a, st);
   }
   // tiles of 64 rows where those of 128 leave CUs without one
   if ((M + 127) / 128 * ((N + 255) / 256) < device_cus())
-    return bf16 ? launch_duo<kDense, kActNone, uint16_t, true, 64>(a, st)
+    return bf16 ? launch_duo<kDense, kActNone, uint16_t, false, 64>(a, st)
                 : launch_duo<kDense, kActNone, float, true, 64>(a, st);
   if (bf16) return launch<kDense, kActNone, uint16_t, false>(a, st);
   return launch_duo<kDense, kActNone, float, true, 128>(a, st);

@@ -25,13 +25,14 @@ constexpr int kMaxRowBlocks = 1 << 20;  // grid bound; rows beyond it by a strid
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kRowWaves * kWave) void quant_rows_kernel(
     const T* __restrict__ src, int64_t rows, int K, int64_t ld, const int32_t* __restrict__ slot,
-    int64_t slots, uint8_t* __restrict__ q, uint8_t* __restrict__ s, float* __restrict__ norm) {
+    const uint8_t* __restrict__ mask, int64_t slots, uint8_t* __restrict__ q, uint8_t* __restrict__ s, float* __restrict__ norm) {
   const int lane = threadIdx.x & (kWave - 1);
   const int pitch = static_cast<int>(q8_pitch(K)), spitch = static_cast<int>(q8_spitch(K));
   for (int64_t r = int64_t(blockIdx.x) * kRowWaves + threadIdx.x / kWave; r < rows;
        r += int64_t(gridDim.x) * kRowWaves) {
     const int64_t to = slot != nullptr ? slot[r] : r;
     if (to < 0 || to >= slots) continue;  // uniform across the wave
+    if (mask != nullptr && mask[r] == 0) continue;
     const T* const row = src + r * ld;
     uint8_t* const qr = q + to * pitch;
     uint8_t* const sr = s + to * spitch;
@@ -141,7 +142,30 @@ __global__ __launch_bounds__(256) void quant_matrix_kernel(const T* __restrict__
 // what is stored; a synchronised token's attention feature goes into its row of
 // the 8-bit attention cache.
 // ---------------------------------------------------------------------------
-template <typename T, int KMAX>
+// One wave per token.  Where the row is loaded from depends on the branch, so a
+// token costs two round trips: what the decision left, then every row's elements
+// (GI groups of 512 a lane's eight of each; GI = 0: any width, a group at a time),
+// all asked for before any is used.
+template <typename T> struct Raw;  // eight elements as loaded; 8-bit rows use the first two words
+template <> struct Raw<uint16_t> {
+  typedef __attribute__((ext_vector_type(4))) unsigned int v;
+  static __device__ __forceinline__ void widen(v x, float* f) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      f[2 * u] = __uint_as_float(x[u] << 16);
+      f[2 * u + 1] = __uint_as_float(x[u] & 0xffff0000u);
+    }
+  }
+};
+template <> struct Raw<float> {
+  typedef __attribute__((ext_vector_type(8))) unsigned int v;
+  static __device__ __forceinline__ void widen(v x, float* f) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) f[u] = __uint_as_float(x[u]);
+  }
+};
+
+template <typename T, int KMAX, int GI>
 __global__ __launch_bounds__(kRowWaves * kWave) void combine_q8_kernel(
     const float* __restrict__ w_t, const int32_t* __restrict__ e_t,
     const int32_t* __restrict__ sigma, const uint8_t* __restrict__ mask,
@@ -151,6 +175,7 @@ __global__ __launch_bounds__(kRowWaves * kWave) void combine_q8_kernel(
     T* __restrict__ out, const T* __restrict__ attn_in, uint8_t* __restrict__ attn_q,
     uint8_t* __restrict__ attn_s, const T* __restrict__ h_sh, int S, int64_t T_tokens, int d,
     int k) {
+  typedef typename Raw<T>::v raw;
   const int lane = threadIdx.x & (kWave - 1);
   const int64_t t = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x)) *
                         int64_t(kRowWaves) +
@@ -170,53 +195,83 @@ __global__ __launch_bounds__(kRowWaves * kWave) void combine_q8_kernel(
       const int64_t f = t * k + p;
       wp[p] = w_t[f];
       slot[p] = sigma[f];
-      from[p] = mask[f] != 0 ? pos[f] : -1;
+      const int at = pos[f];
+      from[p] = mask[f] != 0 ? at : -1;
     }
   }
   const bool syn = attn_in != nullptr && sync[t] != 0;
 
-  for (int c = lane * 8; c < pitch; c += 8 * kWave) {
-    const int n = d - c;  // d is a multiple of 64: eight or none
-    float acc[8];
+  constexpr int G = GI > 0 ? GI : 1;
+  for (int base = 0; base < (GI > 0 ? 1 : pitch); base += 8 * kWave) {
+    raw h[KMAX][G], a[G];
+    int sb[KMAX][G];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) acc[u] = 0.0f;
-    for (int sh = 0; sh < S; ++sh) {
-      float h[8];
-      load8<T, true>(h_sh + (sh * T_tokens + t) * d + c, n, h);
+    for (int gi = 0; gi < G; ++gi) {
+      const int c = base + (gi * kWave + lane) * 8;
+      const bool in = c < d;  // d is a multiple of 64: eight or none
 #pragma unroll
-      for (int u = 0; u < 8; ++u) acc[u] = __fadd_rn(acc[u], h[u]);
+      for (int p = 0; p < KMAX; ++p) {
+        h[p][gi] = raw{};
+        sb[p][gi] = 0;
+        if (p >= k || !in) continue;
+        if (from[p] >= 0) {  // uniform across the wave
+          h[p][gi] = __builtin_nontemporal_load(
+              reinterpret_cast<const raw*>(fresh + int64_t(from[p]) * d + c));
+        } else {
+          const int64_t r = t * k + slot[p];
+          const uint2 q = *reinterpret_cast<const uint2*>(h_c + r * pitch + c);
+          h[p][gi][0] = q.x;
+          h[p][gi][1] = q.y;
+          sb[p][gi] = s_c[r * spitch + c / kBlk];
+        }
+      }
+      a[gi] = raw{};
+      if (syn && in)
+        a[gi] = __builtin_nontemporal_load(reinterpret_cast<const raw*>(attn_in + t * d + c));
     }
 #pragma unroll
-    for (int p = 0; p < KMAX; ++p) {
-      if (p >= k) continue;
-      float h[8];
-      uint8_t* const qr = h_c + (t * k + slot[p]) * pitch + c;
-      uint8_t* const sr = s_c + (t * k + slot[p]) * spitch + c / kBlk;
-      if (from[p] >= 0) {  // uniform across the wave
-        load8<T, true>(fresh + int64_t(from[p]) * d + c, n, h);
-        int byte;
-        const uint2 q = q8_quant8(h, byte);
-        *reinterpret_cast<uint2*>(qr) = q;
-        if ((lane & 15) == 0) *sr = static_cast<uint8_t>(byte);
-        ss[p] += q8_square8(q, byte);
-      } else {
-        const uint2 q = *reinterpret_cast<const uint2*>(qr);
-        const float two = q8_two(*sr);
-        q8_unpack4(q.x, h);
-        q8_unpack4(q.y, h + 4);
+    for (int gi = 0; gi < G; ++gi) {
+      const int c = base + (gi * kWave + lane) * 8;
+      if (c >= pitch) continue;  // whole 16-lane rows in or out
+      float acc[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) h[u] = __fmul_rn(h[u], two);
+      for (int u = 0; u < 8; ++u) acc[u] = 0.0f;
+      for (int sh = 0; sh < S; ++sh) {
+        float v[8];
+        load8<T, true>(h_sh + (sh * T_tokens + t) * d + c, d - c, v);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) acc[u] = __fadd_rn(acc[u], v[u]);
       }
 #pragma unroll
-      for (int u = 0; u < 8; ++u) acc[u] = __fadd_rn(acc[u], __fmul_rn(wp[p], h[u]));
-    }
-    if (n > 0) store8<T, true>(out + t * d + c, n, acc);
-    if (syn) {
-      float a[8];
-      load8<T, true>(attn_in + t * d + c, n, a);
-      int byte;
-      *reinterpret_cast<uint2*>(attn_q + t * pitch + c) = q8_quant8(a, byte);
-      if ((lane & 15) == 0) attn_s[t * spitch + c / kBlk] = static_cast<uint8_t>(byte);
+      for (int p = 0; p < KMAX; ++p) {
+        if (p >= k) continue;
+        float v[8];
+        if (from[p] >= 0) {
+          Raw<T>::widen(h[p][gi], v);
+          int byte;
+          const uint2 q = q8_quant8(v, byte);
+          const int64_t r = t * k + slot[p];
+          *reinterpret_cast<uint2*>(h_c + r * pitch + c) = q;
+          if ((lane & 15) == 0) s_c[r * spitch + c / kBlk] = static_cast<uint8_t>(byte);
+          ss[p] += q8_square8(q, byte);
+        } else {
+          const float two = q8_two(sb[p][gi]);
+          q8_unpack4(h[p][gi][0], v);
+          q8_unpack4(h[p][gi][1], v + 4);
+#pragma unroll
+          for (int u = 0; u < 8; ++u) v[u] = __fmul_rn(v[u], two);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) acc[u] = __fadd_rn(acc[u], __fmul_rn(wp[p], v[u]));
+      }
+      if (c < d) store8<T, true>(out + t * d + c, d - c, acc);
+      if (syn) {
+        float v[8];
+        Raw<T>::widen(a[gi], v);
+        int byte;
+        *reinterpret_cast<uint2*>(attn_q + t * pitch + c) = q8_quant8(v, byte);
+        if ((lane & 15) == 0) attn_s[t * spitch + c / kBlk] = static_cast<uint8_t>(byte);
+      }
     }
   }
 #pragma unroll
@@ -244,12 +299,12 @@ unsigned row_blocks(int64_t rows) {
 }  // namespace
 
 hipError_t launch_quant_rows(const void* src, bool bf16, int64_t rows, int K, int64_t ld,
-                             const int32_t* slot, int64_t slots, uint8_t* q, uint8_t* s,
-                             float* norm, hipStream_t st) {
+                             const int32_t* slot, const uint8_t* mask, int64_t slots, uint8_t* q,
+                             uint8_t* s, float* norm, hipStream_t st) {
   const dim3 grid(row_blocks(rows)), block(kRowWaves * kWave);
 #define MOECA_QROWS(T, V)                                                                        \
   launch_kernel(&quant_rows_kernel<T, V>, grid, block, 0, st, static_cast<const T*>(src), rows, \
-                K, ld, slot, slots, q, s, norm)
+                K, ld, slot, mask, slots, q, s, norm)
   if (bf16) {
     if (vec_rows(src, ld, 2)) MOECA_QROWS(uint16_t, true);
     else MOECA_QROWS(uint16_t, false);
@@ -301,18 +356,17 @@ hipError_t launch_combine_q8(const Shape& s, void* out, const void* attn_in, uin
                              uint8_t* attn_s, const Buffers& b, hipStream_t st) {
   const dim3 grid(static_cast<unsigned>((s.tokens() + kRowWaves - 1) / kRowWaves));
   const dim3 block(kRowWaves * kWave);
-#define MOECA_CQ8(T, KM)                                                                         \
-  launch_kernel(&combine_q8_kernel<T, KM>, grid, block, 0, st, b.w_t, b.e_t, b.sigma, b.mask,    \
+#define MOECA_CQ8(T, KM, GI)                                                                     \
+  launch_kernel(&combine_q8_kernel<T, KM, GI>, grid, block, 0, st, b.w_t, b.e_t, b.sigma, b.mask, \
                 b.sync, b.pos, static_cast<const T*>(b.fresh), static_cast<uint8_t*>(b.h_c),     \
                 b.s_c, b.e_c, b.w_c, b.n_c, static_cast<T*>(out), static_cast<const T*>(attn_in), \
                 attn_q, attn_s, static_cast<const T*>(b.h_sh), s.S, s.tokens(), s.d, s.k)
-  if (s.bf16) {
-    if (s.k <= 2) MOECA_CQ8(uint16_t, 2);
-    else MOECA_CQ8(uint16_t, 8);
-  } else {
-    if (s.k <= 2) MOECA_CQ8(float, 2);
-    else MOECA_CQ8(float, 8);
-  }
+  const int64_t gi = (q8_pitch(s.d) + 8 * kWave - 1) / (8 * kWave);
+  if (s.bf16 && s.k <= 2 && gi <= 2) MOECA_CQ8(uint16_t, 2, 2);
+  else if (s.bf16 && s.k <= 2 && gi <= 4) MOECA_CQ8(uint16_t, 2, 4);
+  else if (s.bf16) MOECA_CQ8(uint16_t, 8, 0);
+  else if (s.k <= 2 && gi <= 2) MOECA_CQ8(float, 2, 2);
+  else MOECA_CQ8(float, 8, 0);
 #undef MOECA_CQ8
   return hipGetLastError();
 }

@@ -60,7 +60,7 @@ int moeca_quant_rows(const void* src, int dtype, int64_t rows, int64_t K, int64_
   if (((reinterpret_cast<uintptr_t>(slot) | reinterpret_cast<uintptr_t>(norm)) & 3u) != 0)
     return fail(MOECA_E_INVAL, "slots and norms must be 4-byte aligned");
   return launched(moeca::launch_quant_rows(src, dtype == MOECA_DTYPE_BF16, rows,
-                                           static_cast<int>(K), ld, slot, slots,
+                                           static_cast<int>(K), ld, slot, nullptr, slots,
                                            static_cast<uint8_t*>(q), static_cast<uint8_t*>(scale),
                                            norm, static_cast<hipStream_t>(stream)),
                   "quantise rows");
@@ -133,8 +133,8 @@ int moeca_quant_linear(const void* x, int dtype, int64_t M, int64_t K, int64_t l
   const auto st = static_cast<hipStream_t>(stream);
   const bool bf16 = dtype == MOECA_DTYPE_BF16;
   const moeca::Q8 v = moeca::q8_view(workspace, M, K);
-  const hipError_t e = moeca::launch_quant_rows(x, bf16, M, static_cast<int>(K), ldx, nullptr, M,
-                                                v.q, v.s, nullptr, st);
+  const hipError_t e = moeca::launch_quant_rows(x, bf16, M, static_cast<int>(K), ldx, nullptr,
+                                                nullptr, M, v.q, v.s, nullptr, st);
   if (e != hipSuccess) return launched(e, "quantise rows");
   return launched(moeca::launch_q8_linear(v, M, static_cast<int>(K), q, scale,
                                           static_cast<int>(N), bias, out, bf16, ldo, st),
