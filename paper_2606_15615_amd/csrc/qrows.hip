@@ -196,10 +196,12 @@ __global__ __launch_bounds__(kRowWaves * kWave) void combine_q8_kernel(
       wp[p] = w_t[f];
       slot[p] = sigma[f];
       const int at = pos[f];
-      from[p] = mask[f] != 0 ? at : -1;
+      // the same for the whole wave: say so, so that branches on it are scalar
+      from[p] = __builtin_amdgcn_readfirstlane(mask[f] != 0 ? at : -1);
     }
   }
-  const bool syn = attn_in != nullptr && sync[t] != 0;
+  const bool syn =
+      __builtin_amdgcn_readfirstlane(attn_in != nullptr && sync[t] != 0 ? 1 : 0) != 0;
 
   constexpr int G = GI > 0 ? GI : 1;
   for (int base = 0; base < (GI > 0 ? 1 : pitch); base += 8 * kWave) {
@@ -363,6 +365,7 @@ hipError_t launch_combine_q8(const Shape& s, void* out, const void* attn_in, uin
                 attn_q, attn_s, static_cast<const T*>(b.h_sh), s.S, s.tokens(), s.d, s.k)
   const int64_t gi = (q8_pitch(s.d) + 8 * kWave - 1) / (8 * kWave);
   if (s.bf16 && s.k <= 2 && gi <= 2) MOECA_CQ8(uint16_t, 2, 2);
+  else if (s.bf16 && s.k <= 2 && gi <= 3) MOECA_CQ8(uint16_t, 2, 3);
   else if (s.bf16 && s.k <= 2 && gi <= 4) MOECA_CQ8(uint16_t, 2, 4);
   else if (s.bf16) MOECA_CQ8(uint16_t, 8, 0);
   else if (s.k <= 2 && gi <= 2) MOECA_CQ8(float, 2, 2);
