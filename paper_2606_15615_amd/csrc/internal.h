@@ -218,11 +218,17 @@ hipError_t launch_quant_matrix(const void* W, bool bf16, int count, int N, int K
 // The combine of a cache8 layer: recomputed rows from b.fresh into the cache.
 hipError_t launch_combine_q8(const Shape& s, void* out, const void* attn_in, uint8_t* attn_q,
                              uint8_t* attn_s, const Buffers& b, hipStream_t st);
-FfnPlan q8_plan(const Shape& s, StepKind kind, int64_t rows);
+// rows: branches the routed experts are expected to have in this step
+FfnPlan q8_plan(const Shape& s, int64_t rows);
 hipError_t launch_q8_up(const Shape& s, int act, const FfnPlan& plan, const QuantWeights& w,
                         const Buffers& b, hipStream_t st);
 hipError_t launch_q8_down(const Shape& s, const FfnPlan& plan, const QuantWeights& w,
                           const Buffers& b, hipStream_t st);
+// The same for at most q8_few_rows() rows straight from the activations.
+int64_t q8_few_rows();
+hipError_t launch_q8_few(const void* x, bool bf16, int64_t M, int K, int64_t ldx, const void* W,
+                         const void* Ws, int N, const float* bias, void* out, int64_t ldo,
+                         hipStream_t st);
 // out = values(x) W^T (+ bias), x of M rows, W of N
 hipError_t launch_q8_linear(const Q8& x, int64_t M, int K, const void* W, const void* Ws, int N,
                             const float* bias, void* out, bool bf16, int64_t ldo,

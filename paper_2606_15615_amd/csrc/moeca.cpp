@@ -471,7 +471,7 @@ int moeca_forward_noalloc(const moeca_layer* L, const void* x, int samples, void
   const moeca_policy& p = L->pol;
   const auto st = static_cast<hipStream_t>(stream);
   moeca::FfnPlan plan =
-      s.experts8 ? moeca::q8_plan(s, moeca::kFullStep, s.branches())
+      s.experts8 ? moeca::q8_plan(s, s.branches())
                  : moeca::ffn_plan(s, moeca::kFullStep, s.branches(), b.part != nullptr);
   if (b.part == nullptr) plan.split_down = 1;
   // the uncached layer: every branch recomputed, no statistic, no cache
@@ -599,7 +599,7 @@ int layer_step(moeca_layer* L, const void* x_t, const void* x_ffn, int t, void* 
   // projection's sums are the same in any tiling.)
   const bool pieces = b.part != nullptr &&
                       !(L->mid_outside && kind != moeca::kRatioStep);
-  const moeca::FfnPlan plan = s.experts8 ? moeca::q8_plan(s, kind, rows)
+  const moeca::FfnPlan plan = s.experts8 ? moeca::q8_plan(s, rows)
                                          : moeca::ffn_plan(s, kind, rows, pieces);
   arm();
   if (!check(moeca::launch_decide(s, sel, budget, p.lambda0, p.lambda1, p.lambda2, !uncached, p.tau0,

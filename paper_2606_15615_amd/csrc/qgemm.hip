@@ -330,9 +330,18 @@ __device__ __forceinline__ void mfma_q8_tied(f32x4_t& c, const i32x8_t& w, const
       : "v"(w), "v"(x), "v"(sw), "v"(sx));
 }
 
+__device__ __forceinline__ void mfma_q8(const Piece<false>& w, const Piece<false>& x, f32x4_t& c) {
+  mfma_q8_tied(c, w.v, x.v, w.s, x.s);
+}
+__device__ __forceinline__ void mfma_q8(const Piece<true>& w, const Piece<true>& x, f32x4_t& c) {
+#pragma unroll
+  for (int h = 0; h < 4; ++h) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.v[h], x.v[h], c, 0, 0, 0);
+}
+
 // ---------------------------------------------------------------------------
-// 128 x 256 tiles: 8 waves (2 x 4) of 64 rows x 64 columns, 4 x 4 tiles of
-// 16 x 16 each (weights the A operand).  A k-tile is 128 bytes of every row, one
+// 128 rows x 256 weight rows for gated up projections, whose block of 128 hidden
+// columns takes 256 weight rows: 8 waves (2 x 4) of 64 x 64, 4 x 4 tiles of 16 x 16
+// each (weights the A operand).  A k-tile is 128 bytes of every row, one
 // block; three of them (48 KB each) are in LDS or on their way, brought by direct
 // global -> LDS loads in the XOR-swizzled order of the bf16 kernels: position p
 // of row r holds 16-byte chunk p ^ ((r >> 1) & 7).  The scales come the same
@@ -353,39 +362,26 @@ constexpr int kMidStage = kMidTileX + kMidTN * kBlk;   // 48 KB
 constexpr int kMidLoadsX = kMidTM / 8 / kMidWaves;     // 2 per wave and stage
 constexpr int kMidLoadsW = kMidTN / 8 / kMidWaves;     // 4
 constexpr int kMidScales = (kMidTM + 2) * 16;          // bytes of a scale buffer: rows, two blocks
-
-__device__ __forceinline__ void mfma_q8(const Piece<false>& w, const Piece<false>& x, f32x4_t& c) {
-  mfma_q8_tied(c, w.v, x.v, w.s, x.s);
-}
-__device__ __forceinline__ void mfma_q8(const Piece<true>& w, const Piece<true>& x, f32x4_t& c) {
-#pragma unroll
-  for (int h = 0; h < 4; ++h) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.v[h], x.v[h], c, 0, 0, 0);
-}
-
-template <int KIND, int ACT, typename T, bool EXACT>
-__global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
-  constexpr bool kGated = ACT == kActSwiglu;
-  constexpr int FM = 4, FN = 4, V = run_columns<KIND, T, FN>();
+template <bool EXACT>
+__global__ __launch_bounds__(kMidThreads, 1) void qgemm_gated_kernel(QArgs a) {
+  constexpr int FM = 4, FN = 4, V = run_columns<kUp, uint8_t, FN>();
   __shared__ __attribute__((aligned(16))) uint8_t lds[kMidStages * kMidStage];
   __shared__ __attribute__((aligned(16))) uint8_t s_sc[2][kMidScales];
   __shared__ int s_src[kMidTM], s_dst[kMidTM];
-  __shared__ __attribute__((aligned(16))) uint32_t s_top[KIND == kUp ? kMidTM : 1][4];
+  __shared__ __attribute__((aligned(16))) uint32_t s_top[kMidTM][4];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wv >> 2, wn = wv & 3;
   const int nt = (a.Nout + kMidTN - 1) / kMidTN;
-  const int total = KIND == kDense ? (a.M + kMidTM - 1) / kMidTM * nt : a.tile_off[a.G];
+  const int total = a.tile_off[a.G];
   const int per = (total + kXcds - 1) / kXcds;
   const int lo = (blockIdx.x % kXcds) * per;
   const int hi = min(total, lo + per);
   const int stride = gridDim.x / kXcds;
-  int toff0 = 0, toff1 = 0;
-  if constexpr (KIND != kDense) {
-    toff0 = lane < a.G ? a.tile_off[lane] : 0x7fffffff;
-    toff1 = lane + 64 < a.G ? a.tile_off[lane + 64] : 0x7fffffff;
-  }
+  const int toff0 = lane < a.G ? a.tile_off[lane] : 0x7fffffff;
+  const int toff1 = lane + 64 < a.G ? a.tile_off[lane + 64] : 0x7fffffff;
   const int KT = a.pitch / kBlk;
   const int nbw = (a.Nout + kBlk - 1) / kBlk;
   const int chunk = (lane & 7) ^ (4 * (wv & 1) + (lane >> 4));
@@ -397,13 +393,10 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
   };
   auto tile = [&](int L) __attribute__((always_inline)) {
     Tile t;
-    int e_base = 0, o0 = 0, cnt = a.M;
-    t.e = 0;
-    if constexpr (KIND != kDense) {
-      t.e = tile_group(L, toff0, toff1, e_base);
-      o0 = a.off[t.e];
-      cnt = a.off[t.e + 1] - o0;
-    }
+    int e_base;
+    t.e = tile_group(L, toff0, toff1, e_base);
+    const int o0 = a.off[t.e];
+    const int cnt = a.off[t.e + 1] - o0;
     const int mt = (cnt + kMidTM - 1) / kMidTM;
     int m, n;
     band_order(L - e_base, mt, nt, m, n);
@@ -424,7 +417,7 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
 #pragma unroll
     for (int u = 0; u < kMidLoadsX; ++u)
       gx[u] = a.X + int64_t(s_src[8 * (wv + kMidWaves * u) + (lane >> 3)]) * a.pitch + chunk * 16;
-    const bool routed = KIND == kDense || t.e < a.E;
+    const bool routed = t.e < a.E;
     const int64_t g = routed ? t.e : t.e - a.E;
     const uint8_t* const W = (routed ? a.W : a.Wsh) + g * a.Nout * a.pitch;
 #pragma unroll
@@ -474,7 +467,7 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
   Tile cur = tile(L);
   {
     int src = 0, dst = -1;
-    if (tid < kMidTM) tile_row<KIND>(a, cur.e, cur.r0, cur.rows, tid, src, dst);
+    if (tid < kMidTM) tile_row<kUp>(a, cur.e, cur.r0, cur.rows, tid, src, dst);
     start(cur, src, dst);
   }
   begin();
@@ -487,7 +480,7 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
     int nsrc = 0, ndst = -1;
     if (has_next) {
       nxt = tile(Ln);
-      if (tid < kMidTM) tile_row<KIND>(a, nxt.e, nxt.r0, nxt.rows, tid, nsrc, ndst);
+      if (tid < kMidTM) tile_row<kUp>(a, nxt.e, nxt.r0, nxt.rows, tid, nsrc, ndst);
     }
     f32x4_t acc[FN][FM];
 #pragma unroll
@@ -563,44 +556,25 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
       start(nxt, nsrc, ndst);
       begin();
     }
-    const int cw = cur.n0 + wn * 64, c0 = cw + 16 * (lane >> 4);
-    if constexpr (KIND == kUp) {
-      const bool whole = cur.n0 + kMidTN <= a.Nout;
+    const int c0 = cur.n0 + wn * 64 + 16 * (lane >> 4);
+    const bool whole = cur.n0 + kMidTN <= a.Nout;
 #pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        f32x4_t* const v[FN] = {&acc[0][i], &acc[1][i], &acc[2][i], &acc[3][i]};
-        const uint32_t top = hidden_row<ACT, FN>(v, c0, a.Nout, whole);
-        if (lane < 16) s_top[wm * 64 + i * 16 + lane][wn] = top;
-      }
-      __syncthreads();
-      static_assert(kGated, "ungated up projections take the other tiles");
-      const int blk = cur.n0 / 2 / kBlk;
-      top4_t tops[FM];
+    for (int i = 0; i < FM; ++i) {
+      f32x4_t* const v[FN] = {&acc[0][i], &acc[1][i], &acc[2][i], &acc[3][i]};
+      const uint32_t top = hidden_row<kActSwiglu, FN>(v, c0, a.Nout, whole);
+      if (lane < 16) s_top[wm * 64 + i * 16 + lane][wn] = top;
+    }
+    __syncthreads();
+    const int blk = cur.n0 / 2 / kBlk;
 #pragma unroll
-      for (int i = 0; i < FM; ++i)
-        tops[i] = *reinterpret_cast<const top4_t*>(s_top[wm * 64 + i * 16 + (lane & 15)]);
-#pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        const int byte =
-            q8_scale_byte(max(max(tops[i][0], tops[i][1]), max(tops[i][2], tops[i][3])));
-        if (drow[i] < 0) continue;
-        f32x4_t* const v[FN] = {&acc[0][i], &acc[1][i], &acc[2][i], &acc[3][i]};
-        store_hidden<ACT, FN>(a.q + int64_t(drow[i]) * a.qpitch, c0, v, q8_inv(byte));
-        if (wn == 0 && lane < 16)
-          a.s[int64_t(drow[i]) * a.qspitch + blk] = static_cast<uint8_t>(byte);
-      }
-    } else {
-      T* const og = static_cast<T*>(KIND == kDense || cur.e < a.E ? a.dst : a.dst_sh);
-      const bool vec =
-          (reinterpret_cast<uintptr_t>(og) & 15u) == 0 && a.ldo * sizeof(T) % 16 == 0;
-      f32x4_t bias[FN];
-      load_bias<FN, V>(a, cw, lane >> 4, bias);
-#pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        if (drow[i] < 0) continue;
-        const f32x4_t* const v[FN] = {&acc[0][i], &acc[1][i], &acc[2][i], &acc[3][i]};
-        store_out<T, FN, V>(a, og + int64_t(drow[i]) * a.ldo, cw, lane >> 4, v, bias, vec);
-      }
+    for (int i = 0; i < FM; ++i) {
+      const top4_t t = *reinterpret_cast<const top4_t*>(s_top[wm * 64 + i * 16 + (lane & 15)]);
+      const int byte = q8_scale_byte(max(max(t[0], t[1]), max(t[2], t[3])));
+      if (drow[i] < 0) continue;
+      f32x4_t* const v[FN] = {&acc[0][i], &acc[1][i], &acc[2][i], &acc[3][i]};
+      store_hidden<kActSwiglu, FN>(a.q + int64_t(drow[i]) * a.qpitch, c0, v, q8_inv(byte));
+      if (wn == 0 && lane < 16)
+        a.s[int64_t(drow[i]) * a.qspitch + blk] = static_cast<uint8_t>(byte);
     }
     if (!has_next) break;
     L = Ln;
@@ -609,10 +583,10 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_mid_kernel(QArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Tiles of TM = 128 or 64 rows by 128 columns (gated: 256 weight rows, TM = 64) in
+// Tiles of TM = 128, 64 or 32 rows by 128 columns (gated: 256 weight rows, TM = 64) in
 // blocks of four waves, two blocks per CU (gated: one): what one block waits for,
 // its loads, its conversions, its epilogue, runs beside the other's matrix
-// instructions.  Waves are 2 x 2 of 64 x 64 (TM = 128) or 1 x 4 of 64 x 32; a ring
+// instructions.  Waves are 2 x 2 of 64 x 64 (TM = 128) or 1 x 4 of TM x 32; a ring
 // of kStages k-tiles, one barrier each, in the swizzled order of the tile above,
 // scales in two buffers of 16 k-tiles.  A tile of TM = 64 skips the 16-row tiles
 // that it has no rows for.
@@ -625,8 +599,8 @@ template <int TM, bool GATED> struct Duo {
   static constexpr int kLoadsX = TM / 8 / kWaves, kLoadsW = TN / 8 / kWaves;
   static constexpr int kScales = (TM + TN / kBlk) * 16;
   static constexpr int kBlocks = GATED ? 1 : 2;
-  static constexpr int kWavesM = TM / 64, kWavesN = kWaves / kWavesM;
-  static constexpr int FM = 4, FN = TN / kWavesN / 16;
+  static constexpr int kWavesM = TM == 128 ? 2 : 1, kWavesN = kWaves / kWavesM;
+  static constexpr int FM = TM / kWavesM / 16, FN = TN / kWavesN / 16;
 };
 
 template <int KIND, int ACT, typename T, bool EXACT, int TM>
@@ -659,7 +633,11 @@ __global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qg
   const int nbw = (a.Nout + kBlk - 1) / kBlk;
   const int chunk = (lane & 7) ^ (4 * (wv & 1) + (lane >> 4));
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(lds) + wv * 1024);
-  const uint32_t sc0 = __builtin_amdgcn_readfirstlane(lds_addr(&s_sc[0][0]) + wv * 1024);
+  // the scales' rows are loaded by the first waves, 64 each, the weight blocks' by
+  // the next one
+  constexpr int kRowWavesX = TM == 128 ? 2 : 1;
+  const uint32_t sc0 = __builtin_amdgcn_readfirstlane(
+      lds_addr(&s_sc[0][0]) + (wv < kRowWavesX ? wv * 1024 : TM * 16));
   const uint32_t fr = (lane & 15) * kBlk + (((lane >> 4) ^ ((lane >> 1) & 7)) * 16);
 
   for (int L = lo + static_cast<int>(blockIdx.x) / kXcds; L < hi; L += stride) {
@@ -700,12 +678,10 @@ __global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qg
         dma16(reinterpret_cast<const uint16_t*>(gx[u] + int64_t(kt) * kBlk),
               lds0 + st * D::kStage + u * D::kWaves * 1024);
     };
-    // scales: the rows' by the first waves, the weight blocks' by the last
     auto issue_scales = [&](int c) __attribute__((always_inline)) {
-      const uint32_t to = __builtin_amdgcn_readfirstlane(sc0 + (c & 1) * D::kScales);
-      if (wv < TM / 64) dma16(reinterpret_cast<const uint16_t*>(gs + c * 16), to);
-      if (wv == TM / 64 && lane < D::TN / kBlk)
-        dma16(reinterpret_cast<const uint16_t*>(gs + c * 16), __builtin_amdgcn_readfirstlane(to));
+      if (wv <= kRowWavesX && lane < (wv < kRowWavesX ? TM : D::TN / kBlk))
+        dma16(reinterpret_cast<const uint16_t*>(gs + c * 16),
+              __builtin_amdgcn_readfirstlane(sc0 + (c & 1) * D::kScales));
     };
     // the weights need no row table: their first k-tiles are asked for before it
     issue_w(0, 0);
@@ -719,7 +695,7 @@ __global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qg
 #pragma unroll
     for (int u = 0; u < D::kLoadsX; ++u)
       gx[u] = a.X + int64_t(s_src[8 * (wv + D::kWaves * u) + (lane >> 3)]) * a.pitch + chunk * 16;
-    gs = wv < TM / 64 ? a.Xs + int64_t(s_src[(64 * wv + lane) & (TM - 1)]) * a.spitch
+    gs = wv < kRowWavesX ? a.Xs + int64_t(s_src[(64 * wv + lane) & (TM - 1)]) * a.spitch
                       : Ws + int64_t(min(n0 / kBlk + (lane & 1), nbw - 1)) * a.spitch;
     issue_scales(0);
 
@@ -779,7 +755,7 @@ __global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qg
     if (n0 + wn * WN >= a.Nout || mine <= 0) run(std::integral_constant<int, 0>{});
     else if (TM == 64 && mine <= 16) run(std::integral_constant<int, 1>{});
     else if (TM == 64 && mine <= 32) run(std::integral_constant<int, 2>{});
-    else run(std::integral_constant<int, 4>{});
+    else run(std::integral_constant<int, FM>{});
     if (!EXACT) {
       asm volatile("s_nop 15\n\ts_nop 15");
 #pragma unroll
@@ -1252,11 +1228,91 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
   slot_wait<0>();  // the last loads have landed before the LDS is given up
 }
 
-template <int KIND, int ACT, typename T, bool EXACT>
-hipError_t launch(const QArgs& a, hipStream_t st) {
-  launch_kernel(&qgemm_mid_kernel<KIND, ACT, T, EXACT>, dim3(device_cus()), dim3(kMidThreads), 0,
-                st, a);
-  return hipGetLastError();
+// ---------------------------------------------------------------------------
+// y = x W^T for up to 16 rows straight from the activations: one launch, no
+// workspace.  A block has 16 columns (weight rows), its four waves every fourth
+// k-tile; a wave loads its weights from memory into the operand registers,
+// quantises the block of every row itself (a lane has 32 of a row's 128 elements),
+// and the waves' sums meet in LDS, added in wave order.  What bounds it is how many
+// loads are in flight: at M = 1 the grid covers every CU from N = 4096 on, and all
+// of a wave's loads up to K = 1536 are asked for at once.
+// ---------------------------------------------------------------------------
+constexpr int kFewWaves = 4;
+constexpr int kFewAhead = 3;  // k-tiles of a wave in flight
+
+template <typename T, bool VEC>
+__global__ __launch_bounds__(kFewWaves * kWave) void qlinear_few_kernel(
+    const T* __restrict__ x, int M, int K, int64_t ldx, const uint8_t* __restrict__ W,
+    const uint8_t* __restrict__ Ws, int N, const float* __restrict__ bias, T* __restrict__ out,
+    int64_t ldo) {
+  __shared__ f32x4_t s_acc[kFewWaves - 1][kWave];
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wv = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+  const int g = lane >> 4, r = lane & 15;
+  const int pitch = static_cast<int>(q8_pitch(K)), spitch = static_cast<int>(q8_spitch(K));
+  const int KT = pitch / kBlk;
+  const int n0 = blockIdx.x * 16;
+  const uint8_t* const wrow = W + int64_t(min(n0 + r, N - 1)) * pitch + g * 16;
+  const uint8_t* const wsc = Ws + int64_t(n0 / kBlk) * spitch;
+  const bool in = r < M;
+  const T* const xr = x + int64_t(in ? r : 0) * ldx;  // lanes without a row: the first, as zeros
+  f32x4_t acc{0.0f, 0.0f, 0.0f, 0.0f};
+
+  for (int k0 = wv; k0 < KT; k0 += kFewWaves * kFewAhead) {
+    u32x4_t w[kFewAhead][2];
+    int sw[kFewAhead];
+    float v[kFewAhead][32];
+#pragma unroll
+    for (int t = 0; t < kFewAhead; ++t) {
+      const int kt = k0 + kFewWaves * t;
+      if (kt >= KT) continue;  // uniform
+      w[t][0] = *reinterpret_cast<const u32x4_t*>(wrow + int64_t(kt) * kBlk);
+      w[t][1] = *reinterpret_cast<const u32x4_t*>(wrow + int64_t(kt) * kBlk + 64);
+      sw[t] = wsc[kt];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        const int c = kt * kBlk + 64 * (h >> 1) + g * 16 + 8 * (h & 1);
+        load8<T, VEC>(xr + c, K - c, &v[t][8 * h]);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < kFewAhead; ++t) {
+      if (k0 + kFewWaves * t >= KT) continue;
+      Piece<true> pw, px;
+      pw.set(w[t][0], w[t][1], sw[t]);
+      const float* const e = v[t];
+      uint32_t top = 0;
+#pragma unroll
+      for (int u = 0; u < 32; ++u) top = max(top, q8_mag(e[u]));
+      if (__builtin_expect(__any(top >= kInfBits), 0)) {
+        top = 0;
+#pragma unroll
+        for (int u = 0; u < 32; ++u) top = max(top, q8_finite(e[u]));
+      }
+      const int byte = q8_scale_byte(quad_max(top));
+      const float inv = q8_inv(byte);
+      u32x4_t q[2];
+#pragma unroll
+      for (int d = 0; d < 8; ++d)
+        q[d >> 2][d & 3] = in ? q8_pack4(e[4 * d] * inv, e[4 * d + 1] * inv, e[4 * d + 2] * inv,
+                                         e[4 * d + 3] * inv)
+                              : 0u;
+      px.set(q[0], q[1], byte);
+      mfma_q8(pw, px, acc);
+    }
+  }
+  if (wv > 0) s_acc[wv - 1][lane] = acc;
+  __syncthreads();
+  if (wv > 0 || !in) return;
+#pragma unroll
+  for (int w = 0; w < kFewWaves - 1; ++w) acc += s_acc[w][lane];
+  const int c = n0 + 4 * g;
+  T* const o = out + int64_t(r) * ldo;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    if (c + u >= N) continue;
+    o[c + u] = Act<T>::from_f32(bias != nullptr ? acc[u] + bias[c + u] : acc[u]);
+  }
 }
 
 template <int KIND, int ACT, typename T>
@@ -1276,14 +1332,19 @@ hipError_t launch_duo(const QArgs& a, hipStream_t st) {
 template <int ACT>
 hipError_t launch_up(const QArgs& a, bool exact, const FfnPlan& plan, hipStream_t st) {
   if (plan.tall_up) return launch_tall<kUp, ACT, float>(a, st);
-  if (plan.tm_up == 64)
-    return exact ? launch_duo<kUp, ACT, float, true, 64>(a, st)
-                 : launch_duo<kUp, ACT, float, false, 64>(a, st);
-  if constexpr (ACT == kActSwiglu)
-    return exact ? launch<kUp, ACT, float, true>(a, st) : launch<kUp, ACT, float, false>(a, st);
-  else
-    return exact ? launch_duo<kUp, ACT, float, true, 128>(a, st)
-                 : launch_duo<kUp, ACT, float, false, 128>(a, st);
+  if (plan.tm_up == 128) {
+    if constexpr (ACT == kActSwiglu) {
+      const dim3 grid(device_cus()), block(kMidThreads);
+      if (exact) launch_kernel(&qgemm_gated_kernel<true>, grid, block, 0, st, a);
+      else launch_kernel(&qgemm_gated_kernel<false>, grid, block, 0, st, a);
+      return hipGetLastError();
+    } else {
+      return exact ? launch_duo<kUp, ACT, float, true, 128>(a, st)
+                   : launch_duo<kUp, ACT, float, false, 128>(a, st);
+    }
+  }
+  return exact ? launch_duo<kUp, ACT, float, true, 64>(a, st)
+               : launch_duo<kUp, ACT, float, false, 64>(a, st);
 }
 
 // Whether the 256 x 256 tiles can take a product: rows addressed by 32-bit byte
@@ -1294,6 +1355,43 @@ bool tall_capable(int64_t rows, int K) {
 
 // Whether the up projection takes the exact products (above).
 bool exact_up(const Shape& s) { return !s.bf16 || s.cache8; }
+
+// The tile height (32, 64, 128, or 256 for the 256-column tiles) that takes least
+// time: blocks come in rounds of two per CU, the last one perhaps of one, which is
+// over sooner; the 256-column tiles one per CU.  Times of a round in tenths of a
+// microsecond, per k-tile and fixed, one block and two per CU, fitted to dense
+// products of 17 to 16384 rows, 640 to 4608 columns, K 640 to 9216: of 84 bf16 sizes
+// the tile chosen is the fastest but for a few within 8 %.  Measured, us, 32 / 64 /
+// 128 rows / 256 columns: 129 x 1152 x 4608 9.7 11.0 13.4 19.6; 700 x 4608 x 4608
+// 44 33 37 48; 1500 x 1152 x 4608 25.3 22.2 19.5 23.9; 8192 x 4608 x 4608
+// 320 229 189 179.
+// tiles(tm, tn): tiles of a height and width; least: the lowest height there is.
+template <typename F>
+int q8_tile(F tiles, int kt, bool exact, bool tall, int least) {
+  struct Cost {
+    int tm, one_kt, one, two_kt, two;
+  };
+  constexpr Cost kFast[3] = {{32, 37, 370, 62, 260}, {64, 60, 300, 74, 430}, {128, 67, 500, 98, 340}};
+  constexpr Cost kExact[3] = {{32, 53, 350, 87, 380}, {64, 77, 390, 108, 680}, {128, 140, 480, 187, 660}};
+  const int64_t cus = device_cus();
+  int best = 0;
+  int64_t cost = 0;
+  for (const Cost& c : exact ? kExact : kFast) {
+    if (c.tm < least) continue;
+    const int64_t n = tiles(c.tm, 128), rest = n % (2 * cus);
+    const int64_t one = c.one_kt * kt + c.one, two = c.two_kt * kt + c.two;
+    const int64_t t = n / (2 * cus) * two + (rest == 0 ? 0 : rest <= cus ? one : two);
+    if (best == 0 || t < cost) {
+      best = c.tm;
+      cost = t;
+    }
+  }
+  if (tall) {
+    const int64_t t = (tiles(kTallTM, kTallTN) + cus - 1) / cus * (123 * kt + 1040);
+    if (t < cost) best = kTallTM;
+  }
+  return best;
+}
 
 }  // namespace
 
@@ -1307,27 +1405,28 @@ Q8 q8_view(void* base, int64_t rows, int64_t K) {
   return Q8{p, p + (rows * q8_pitch(K) + 255) / 256 * 256};
 }
 
-FfnPlan q8_plan(const Shape& s, StepKind kind, int64_t rows) {
-  (void)kind;
+FfnPlan q8_plan(const Shape& s, int64_t rows) {
   FfnPlan p;
-  p.tm = p.tm_up = 128;
-  const int64_t mean = rows / s.E;
-  const bool many = mean >= 144, few = mean <= 48, exact = exact_up(s);
-  p.tn_up = s.swiglu ? kMidTN : 128;
-  p.tn_down = s.bf16 ? kMidTN : 128;
-  p.tall_up = many && !exact && tall_capable(s.tokens(), s.d);
-  p.tall_down = many && s.bf16 && tall_capable(s.mid_rows(), s.d_ff);
+  const bool exact = exact_up(s);
+  // the rows of an expert vary: an eighth above the mean
+  const int64_t mean = rows / s.E + rows / s.E / 8;
+  auto tiles = [&](int n) {
+    return [&s, mean, n](int tm, int tn) {
+      return (s.E * std::max<int64_t>(1, (mean + tm - 1) / tm) +
+              s.S * ((s.tokens() + tm - 1) / tm)) * ((n + tn - 1) / tn);
+    };
+  };
+  const int ku = static_cast<int>(q8_pitch(s.d) / kBlk), kd = static_cast<int>(q8_pitch(s.d_ff) / kBlk);
+  p.tm_up = q8_tile(tiles(s.up_rows()), ku, exact, !exact && tall_capable(s.tokens(), s.d), 64);
+  p.tm = q8_tile(tiles(s.d), kd, !s.bf16, s.bf16 && tall_capable(s.mid_rows(), s.d_ff), 64);
+  p.tall_up = p.tm_up == kTallTM;
+  p.tall_down = p.tm == kTallTM;
+  // gated: 64-row tiles, one block per CU, for few rows only
+  if (s.swiglu && !p.tall_up) p.tm_up = mean <= 48 ? 64 : kMidTM;
+  p.tn_up = p.tall_up || s.swiglu ? 256 : 128;
+  p.tn_down = p.tall_down ? kTallTN : 128;
   p.half_up = !s.swiglu;
   p.half_down = true;
-  if (p.tall_up) {
-    p.tm_up = kTallTM;
-    p.tn_up = kTallTN;
-  }
-  if (p.tall_down) p.tm = kTallTM;
-  if (few) {
-    p.tm_up = p.tm = 64;
-    p.tn_down = 128;
-  }
   return p;
 }
 
@@ -1390,8 +1489,32 @@ hipError_t launch_q8_down(const Shape& s, const FfnPlan& plan, const QuantWeight
   if (plan.tm == 64)
     return s.bf16 ? launch_duo<kDown, kActNone, uint16_t, false, 64>(a, st)
                   : launch_duo<kDown, kActNone, float, true, 64>(a, st);
-  if (s.bf16) return launch<kDown, kActNone, uint16_t, false>(a, st);
-  return launch_duo<kDown, kActNone, float, true, 128>(a, st);
+  return s.bf16 ? launch_duo<kDown, kActNone, uint16_t, false, 128>(a, st)
+                : launch_duo<kDown, kActNone, float, true, 128>(a, st);
+}
+
+int64_t q8_few_rows() { return 16; }
+
+hipError_t launch_q8_few(const void* x, bool bf16, int64_t M, int K, int64_t ldx, const void* W,
+                         const void* Ws, int N, const float* bias, void* out, int64_t ldo,
+                         hipStream_t st) {
+  if (M > q8_few_rows()) return hipErrorInvalidValue;
+  const dim3 grid(static_cast<unsigned>((N + 15) / 16)), block(kFewWaves * kWave);
+  const size_t elem = bf16 ? 2 : 4;
+  const bool vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && ldx * elem % 16 == 0;
+#define MOECA_FEW(T, V)                                                                      \
+  launch_kernel(&qlinear_few_kernel<T, V>, grid, block, 0, st, static_cast<const T*>(x),     \
+                static_cast<int>(M), K, ldx, static_cast<const uint8_t*>(W),                 \
+                static_cast<const uint8_t*>(Ws), N, bias, static_cast<T*>(out), ldo)
+  if (bf16) {
+    if (vec) MOECA_FEW(uint16_t, true);
+    else MOECA_FEW(uint16_t, false);
+  } else {
+    if (vec) MOECA_FEW(float, true);
+    else MOECA_FEW(float, false);
+  }
+#undef MOECA_FEW
+  return hipGetLastError();
 }
 
 hipError_t launch_q8_linear(const Q8& x, int64_t M, int K, const void* W, const void* Ws, int N,
@@ -1409,17 +1532,21 @@ hipError_t launch_q8_linear(const Q8& x, int64_t M, int K, const void* W, const 
   a.ldo = ldo;
   a.bias = bias;
   a.dst = out;
-  if (bf16 && M >= 256 && tall_capable(M, K)) {
-    a.dense_tm = tall_rows_one(M, (N + kTallTN - 1) / kTallTN, device_cus());
-    a.dense_half = 0;
-    return launch_tall<kDense, kActNone, uint16_t>(a, st);
+  auto tiles = [&](int tm, int tn) { return (M + tm - 1) / tm * ((int64_t(N) + tn - 1) / tn); };
+  switch (q8_tile(tiles, a.pitch / kBlk, !bf16, bf16 && tall_capable(M, K), 32)) {
+    case 32:
+      return bf16 ? launch_duo<kDense, kActNone, uint16_t, false, 32>(a, st)
+                  : launch_duo<kDense, kActNone, float, true, 32>(a, st);
+    case 64:
+      return bf16 ? launch_duo<kDense, kActNone, uint16_t, false, 64>(a, st)
+                  : launch_duo<kDense, kActNone, float, true, 64>(a, st);
+    case 128:
+      return bf16 ? launch_duo<kDense, kActNone, uint16_t, false, 128>(a, st)
+                  : launch_duo<kDense, kActNone, float, true, 128>(a, st);
+    default:
+      a.dense_tm = tall_rows_one(M, (N + kTallTN - 1) / kTallTN, device_cus());
+      return launch_tall<kDense, kActNone, uint16_t>(a, st);
   }
-  // tiles of 64 rows where those of 128 leave CUs without one
-  if ((M + 127) / 128 * ((N + 255) / 256) < device_cus())
-    return bf16 ? launch_duo<kDense, kActNone, uint16_t, false, 64>(a, st)
-                : launch_duo<kDense, kActNone, float, true, 64>(a, st);
-  if (bf16) return launch<kDense, kActNone, uint16_t, false>(a, st);
-  return launch_duo<kDense, kActNone, float, true, 128>(a, st);
 }
 
 }  // namespace moeca

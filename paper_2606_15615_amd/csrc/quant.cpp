@@ -132,6 +132,10 @@ int moeca_quant_linear(const void* x, int dtype, int64_t M, int64_t K, int64_t l
                                    std::to_string(bytes));
   const auto st = static_cast<hipStream_t>(stream);
   const bool bf16 = dtype == MOECA_DTYPE_BF16;
+  if (M <= moeca::q8_few_rows())
+    return launched(moeca::launch_q8_few(x, bf16, M, static_cast<int>(K), ldx, q, scale,
+                                         static_cast<int>(N), bias, out, ldo, st),
+                    "quantised product");
   const moeca::Q8 v = moeca::q8_view(workspace, M, K);
   const hipError_t e = moeca::launch_quant_rows(x, bf16, M, static_cast<int>(K), ldx, nullptr,
                                                 nullptr, M, v.q, v.s, nullptr, st);
