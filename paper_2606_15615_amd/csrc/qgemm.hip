@@ -57,9 +57,9 @@ struct QArgs {
   int E, G, k;     // routed groups, all groups, branches a token
   int M;           // dense: rows
   // of the 256-column tiles: rows, at most, and (tm[2]) whether they are 128
-  // columns wide (from the lists kernel; dense: from the host)
+  // columns wide (from the lists kernel; dense: rows from the host)
   const int32_t* tm;
-  int dense_tm, dense_half;
+  int dense_tm;
   int pitch, spitch;
   int Nout;        // weight rows of a group
   int64_t ldo;     // elements of an output row (down, dense)
@@ -347,10 +347,10 @@ __device__ __forceinline__ void mfma_q8(const Piece<true>& w, const Piece<true>&
 // of row r holds 16-byte chunk p ^ ((r >> 1) & 7).  The scales come the same
 // way, 16 bytes (16 k-tiles) of each row at a time, into one of two buffers; a
 // k-tile's are read as bytes.  The two groups are the tile's halves of rows; EXACT
-// converts its operands in the memory slot.  An up projection's block of 128 hidden columns
-// lies with two waves of a row (gated: four), which exchange their largest
-// magnitudes through LDS.  Persistent, one block per CU; the next tile's first
-// loads start before this tile's epilogue.
+// converts its operands in the memory slot.  A block of 128 hidden columns lies
+// with four waves of a row, which exchange their largest magnitudes through LDS.
+// Persistent, one block per CU; the next tile's first loads start before this
+// tile's epilogue.
 // ---------------------------------------------------------------------------
 constexpr int kMidTM = 128;
 constexpr int kMidTN = 256;
@@ -587,7 +587,7 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_gated_kernel(QArgs a) {
 // blocks of four waves, two blocks per CU (gated: one): what one block waits for,
 // its loads, its conversions, its epilogue, runs beside the other's matrix
 // instructions.  Waves are 2 x 2 of 64 x 64 (TM = 128) or 1 x 4 of TM x 32; a ring
-// of kStages k-tiles, one barrier each, in the swizzled order of the tile above,
+// of kStages k-tiles, one barrier each, in the swizzled order of the gated kernel,
 // scales in two buffers of 16 k-tiles.  A tile of TM = 64 skips the 16-row tiles
 // that it has no rows for.
 // ---------------------------------------------------------------------------
@@ -815,8 +815,8 @@ __global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qg
 
 // ---------------------------------------------------------------------------
 // 256 x 256 tiles for many rows, 8-bit products only: 64 KB of a k-tile per 16.8
-// MFLOP instead of 48 KB per 8.4 (the tile above), so that neither what a CU can
-// load nor its LDS bounds the matrix instructions.
+// MFLOP, where 128 x 128 take 32 KB per 4.2 and 128 x 256 take 48 KB per 8.4, so
+// that neither what a CU can load nor its LDS bounds the matrix instructions.
 //
 // The schedule is the 256 x 256 bf16 kernel's (ffn.hip), whose k-tile has the
 // same bytes: eight waves of 128 rows x 64 columns (2 x 4), two LDS buffers of a
@@ -872,7 +872,7 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wv >> 2, wn = wv & 3;  // wm is also the ping-pong group
   const int TM = kTable ? a.tm[0] : a.dense_tm;
-  const bool half = !kGated && (kTable ? a.tm[2] : a.dense_half) != 0;
+  const bool half = kTable && !kGated && a.tm[2] != 0;
   const int TN = half ? 128 : kTallTN;
   const int nt = (a.Nout + TN - 1) / TN;
   const int total = kTable ? a.tile_off[a.G] : (a.M + TM - 1) / TM * nt;

@@ -273,6 +273,7 @@ class Case:
                  "ratio": _lib.MOECA_MODE_RATIO}
         self.d, self.E, self.k, self.B, self.N, self.act, self.S = d, E, k, B, N, act, S
         self.dtype, self.experts, self.cache, self.T = dtype, experts, cache, B * N
+        self.mode = mode
         g = self.g = np.random.default_rng(seed)
         U = d_ff * (2 if act == "swiglu" else 1)
         self.L = MoecaLayer(d, E, k, d_ff, batch=B, tokens=N, mode=modes[mode], act=act,
@@ -331,6 +332,10 @@ class Case:
         x, x64 = _t(self.x.reshape(self.B, self.N, d), self.dtype)
         x64 = x64.reshape(T, d)
         before = self.state() if cached else None
+        if not cached and self.mode != "full":
+            plain = self.L.read("h_c").reshape(T, k, d)
+            if self.dtype == "bf16":
+                plain = (plain.astype(np.uint32) << 16).view(np.float32)
         if self.attn is not None:
             a, a64 = _t(self.g.normal(size=(self.B, self.N, d)), self.dtype)
             self.attn_in.copy_(a)
@@ -347,8 +352,8 @@ class Case:
             r, p = np.nonzero((e == i) & mask)
             if len(r):
                 h[r, p], tol[r, p] = self.ffn(x64[r], self.up[i], self.down[i], exact)
-        if cached:
-            old = Q.row_values(before["q"], before["s"], d).reshape(T, k, d)
+        if cached or self.mode != "full":
+            old = Q.row_values(before["q"], before["s"], d).reshape(T, k, d) if cached else plain
             r, p = np.nonzero(~mask)
             h[r, p] = old[r, sig[r, p]]
         want = (w[:, :, None] * h).sum(1)
@@ -587,3 +592,80 @@ def test_far_slots():
     c.write(x, slot)
     np.testing.assert_array_equal(c.read(slot).double().cpu().numpy(), Q.round_trip(x64))
     assert int(c.q.view(torch.int32).count_nonzero()) <= 3 * K // 4
+
+
+# ---- every tile -------------------------------------------------------------------
+@pytest.mark.parametrize("M,K,N,extra,bias", [
+    # five blocks of K, the fewest that the 256-column tiles are chosen for; 17, 31, 32
+    # and 33: pieces of 16 scales; columns that end inside a half and unaligned rows
+    (4000, 640, 3900, 0, True), (2049, 2176, 4609, 0, False), (3300, 3968, 2570, 6, True),
+    (5000, 4096, 2307, 5, False), (3500, 4224, 2500, 12, True),
+    # 128-row tiles
+    (1000, 4608, 4608, 0, True), (8192, 700, 2050, 2, False)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_linear_many_rows(M, K, N, extra, bias, dtype):
+    """The larger tiles; the 64-bit products are the GPU's own."""
+    import torch
+    from paper_2606_15615_amd import quant
+    say(f"  linear {M} x {K} x {N} stride +{extra} bias {bias} {dtype}")
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(M + K + N)
+
+    def rnd(*s):
+        return torch.randn(*s, generator=gen, device="cuda:0")
+    x = rnd(M, K) * torch.exp(2 * rnd(M, 1))
+    x = x.bfloat16() if dtype == "bf16" else x
+    w = (rnd(N, K) / K ** 0.5).bfloat16()
+    b = rnd(N) if bias else None
+    W = quant.quantize_matrix(w)
+    rows = quant.QuantRows(M, K)
+    rows.write(x)
+    xv = rows.read(dtype=torch.float32).double()       # exact
+    sc = W.scale[:, :(K + 127) // 128].double()
+    wv = W.q.view(torch.float8_e4m3fn)[:, :K].double() * torch.exp2(
+        sc.repeat_interleave(128, 1)[:, :K].repeat_interleave(128, 0)[:N] - 127)
+    big = torch.full((M, N + extra), 9.0, dtype=x.dtype, device="cuda:0")
+    out = big[:, :N]
+    quant.linear(x, W, b, out=out)
+    want = xv @ wv.t()
+    mag = xv.abs() @ wv.abs().t()
+    if bias:
+        want += b.double()
+    tol = (K + 9) * U32 * (mag + want.abs()) + (U16 if dtype == "bf16" else U32) * want.abs()
+    if dtype == "bf16":
+        tol += GROUP * mag
+    err = (out.double() - want).abs()
+    say(f"    largest share of the bound {float((err / tol).max()):.3f}")
+    assert bool((err <= tol).all())
+    assert bool((big[:, N:] == 9.0).all())
+
+
+TILES = [
+    # 256 x 256 tiles up and down, full ones and (threshold steps) 128 columns wide;
+    # the 128-row tiles for exact products
+    (dict(d=1536, E=8, k=2, d_ff=1536, B=1, N=4000), "experts"),
+    (dict(d=1536, E=8, k=2, d_ff=1536, B=1, N=4000), "both"),
+    (dict(d=640, E=8, k=2, d_ff=1472, B=1, N=4096, act="gelu_erf"), "experts"),
+    # gated: 256 x 256, 128 x 256, and 128 x 256 exact; hidden widths that end in a block
+    (dict(d=1664, E=8, k=2, d_ff=640, B=3, N=1100, act="swiglu", S=1), "experts"),
+    (dict(d=1536, E=8, k=2, d_ff=768, B=1, N=4000, act="swiglu"), "both"),
+    (dict(d=256, E=4, k=2, d_ff=192, B=1, N=400, act="swiglu"), "experts"),
+    (dict(d=256, E=4, k=2, d_ff=320, B=1, N=400, act="swiglu", dtype="fp32"), "both"),
+    # 128-row tiles, exact up and down
+    (dict(d=640, E=8, k=2, d_ff=1280, B=2, N=1500, dtype="fp32"), "experts"),
+    # small ones over a plain cache
+    (dict(d=192, E=8, k=2, d_ff=320, B=2, N=77), "experts"),
+    (dict(d=320, E=16, k=3, d_ff=192, B=3, N=61, act="swiglu", S=2), "experts"),
+]
+
+
+@pytest.mark.parametrize("i", range(len(TILES)))
+def test_layer_tiles(i):
+    """Full steps, steps that recompute next to nothing and steps that recompute
+    most, over tiles of every size, with the plain and the 8-bit cache."""
+    kw, form = TILES[i]
+    say(f"  {form}: {kw}")
+    c = Case(**kw, mode="threshold", tau0=8.0, cache=form == "both", seed=40 + i, attention=False)
+    for t in range(3):
+        c.step(t, form)
+        c.drift(0.02 if t == 0 else 0.6)
