@@ -1072,7 +1072,7 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
         constexpr int nx = kTail || NX == 4 ? 256 : NX == 2 ? 192 : 128;
         const int so = __builtin_amdgcn_readfirstlane(sc * kTallScales + (t & 15));
         auto settle = [&]() __attribute__((always_inline)) {
-          slot_wait<kTail ? 8 : 8 + NX>();
+          slot_wait<kTail ? 8 : (CA ? 8 : 4) + NX>();
           slot_barrier();
         };
         // phase 0: X0 x W0
@@ -1094,7 +1094,7 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
           read_x(b, 1, NX);
           read_sx(so, 1, NX);
         }
-        issue_w(lt, b, 1);
+        if (CA || kTail) issue_w(lt, b, 1);
         settle();
         if (CA && NX > 0) mfma_q(1, 1, q);
         slot_barrier();
