@@ -350,7 +350,10 @@ __device__ __forceinline__ void mfma_q8(const Piece<true>& w, const Piece<true>&
 // converts its operands in the memory slot.  A block of 128 hidden columns lies
 // with four waves of a row, which exchange their largest magnitudes through LDS.
 // Persistent, one block per CU; the next tile's first loads start before this
-// tile's epilogue.
+// tile's epilogue.  Measured, 64 experts of 2048 x 1408, 4 x 1024 tokens, eight
+// branches each: 256 us with the quantising of x, 1.48 PFLOP/s (EXACT 451 us, 0.84
+// PFLOP/s: the conversions fill the memory slot).  Two blocks of 64 x 256 a CU do not
+// fit its LDS, and one took longer than this from some 50 rows an expert on.
 // ---------------------------------------------------------------------------
 constexpr int kMidTM = 128;
 constexpr int kMidTN = 256;
@@ -590,6 +593,13 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_gated_kernel(QArgs a) {
 // of kStages k-tiles, one barrier each, in the swizzled order of the gated kernel,
 // scales in two buffers of 16 k-tiles.  A tile of TM = 64 skips the 16-row tiles
 // that it has no rows for.
+//
+// What bounds it: with many rows, EXACT, what a CU can load (20 bytes a clock; 16
+// experts of 1152 x 4608, 8 x 1024 tokens, up 206 us, 0.85 PFLOP/s of bf16
+// instructions); with few, the stream of the weights (256 tokens of the same layer: up
+// 85 MB in 21 to 25 us, 576 tiles for 512 places; down 20.5 us, 4.1 TB/s).  A ring of
+// six k-tiles instead of three left down at 21 and slowed up to 33 us (one block per
+// CU).  Dense 333 x 1152 x 4608 10.9 us, 1000 rows 17.6 us.
 // ---------------------------------------------------------------------------
 template <int TM, bool GATED> struct Duo {
   static constexpr int TN = GATED ? 256 : 128;
@@ -834,7 +844,16 @@ __global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qg
 // The rows of a tile, 256, 192 or 128, come from the lists kernel's table (dense:
 // from the host) as for the bf16 kernel, and so do its columns: 128 where tiles of
 // 256 would leave half of the CUs without one (a cache step that recomputes few
-// branches, which the host cannot know).
+// branches, which the host cannot know); the second columns' region is not loaded
+// then (a cycle's down projections 49.1 -> 46.5 us on average).
+//
+// Measured: 16384 x 4608 x 4608 300 us, 2.3 PFLOP/s; 16 experts of 1152 x 4608, 8 x
+// 1024 tokens, up 180 us and down 98 us, 0.97 and 1.77 PFLOP/s; 64 gated experts of
+// 2048 x 1408, 4 x 4096 tokens, up 930 us and down 615 us, 2.0 and 1.5 PFLOP/s.  A
+// k-tile takes 1.2 to 1.4 us a tile (the matrix instructions alone 0.9), a tile some 10 us
+// besides: 128 KB of results leave every CU at about the same time.  Letting the next
+// tile's counted waits pass those stores changed nothing (340 and 340 us with
+// the quantising).
 // ---------------------------------------------------------------------------
 constexpr int kTallTM = 256;
 constexpr int kTallTN = 256;
@@ -1235,7 +1254,8 @@ __global__ __launch_bounds__(kTallThreads, 1) void qgemm_tall_kernel(QArgs a) {
 // quantises the block of every row itself (a lane has 32 of a row's 128 elements),
 // and the waves' sums meet in LDS, added in wave order.  What bounds it is how many
 // loads are in flight: at M = 1 the grid covers every CU from N = 4096 on, and all
-// of a wave's loads up to K = 1536 are asked for at once.
+// of a wave's loads up to K = 1536 are asked for at once.  1 x 1152 x 4608 6.6 us, 16
+// rows 7.3 us; quantising first, then 64-row tiles, takes 7.8 and 8.4 us.
 // ---------------------------------------------------------------------------
 constexpr int kFewWaves = 4;
 constexpr int kFewAhead = 3;  // k-tiles of a wave in flight

@@ -5,7 +5,10 @@
 // on one side and K + K / 128 on the other.  One wavefront per row, eight
 // elements a lane, so that a block of 128 is one 16-lane row of the wave and
 // its largest magnitude four DPP steps; every element is loaded once and kept
-// in registers between the maximum and the conversion.
+// in registers between the maximum and the conversion.  Measured, 16384 rows of
+// 1152, bf16: written with their norms in 12.9 us, 4.4 TB/s; read in 12.0 us, 4.7 TB/s
+// (a copy of 1 GiB: 5.2).  Asking for three groups of a row before using the first
+// took 0.8 us more.  154 rows take 4.2 us, a launch and two round trips.
 #include <algorithm>
 
 #include "common.h"
@@ -84,7 +87,8 @@ __global__ __launch_bounds__(kRowWaves * kWave) void dequant_rows_kernel(
 
 // Weights [count][N][K] (dense) to q [count][N][pitch], s [count][ceil(N / 128)]
 // [spitch]: a block per 128 x 128 of a matrix, its 64 elements a thread kept in
-// registers between the maximum and the conversion.
+// registers between the maximum and the conversion.  16 x 4608 x 1152, bf16: 50 us,
+// 5.1 TB/s.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void quant_matrix_kernel(const T* __restrict__ W, int N, int K,
                                                            uint8_t* __restrict__ q,
@@ -145,7 +149,9 @@ __global__ __launch_bounds__(256) void quant_matrix_kernel(const T* __restrict__
 // One wave per token.  Where the row is loaded from depends on the branch, so a
 // token costs two round trips: what the decision left, then every row's elements
 // (GI groups of 512 a lane's eight of each; GI = 0: any width, a group at a time),
-// all asked for before any is used.
+// all asked for before any is used.  8192 tokens of 1152, two branches: a full step
+// 32 us (104 MB), a cache step 17.5 us, of five waves a SIMD; six (80 registers) 1.4 us
+// more, eight (64, spilled) 12 us more.
 template <typename T> struct Raw;  // eight elements as loaded; 8-bit rows use the first two words
 template <> struct Raw<uint16_t> {
   typedef __attribute__((ext_vector_type(4))) unsigned int v;
