@@ -134,7 +134,8 @@ int moeca_layer_set_shared(moeca_layer* layer, const void* W_up_s, const void* W
  *   MOECA_QUANT_EXPERTS  the step quantises its FFN input, multiplies 8-bit
  *     operands, and quantises each expert's hidden rows act(W_up x) from their
  *     fp32 values; the down projection's rows are of the policy dtype as
- *     before.  Shared experts are held the same way, the router is not.  The
+ *     before.  Products are those of moeca_quant_linear() in the policy dtype, but
+ *     exact for the hidden rows of layers with MOECA_QUANT_CACHE.  Shared experts are held the same way, the router is not.  The
  *     weights are bound with moeca_layer_set_weights_quant() (and
  *     moeca_layer_set_shared_quant()) in the place of the plain calls.
  *   MOECA_QUANT_CACHE    cached branch rows are 8-bit, their norms those of the
@@ -392,7 +393,10 @@ int moeca_quant_matrix(const void* W, int dtype, int64_t count, int64_t N, int64
 /* out = x W^T (+ bias) for rows x [M][K] of the activation type, quantised by
  * the call, and a quantised matrix W of N rows: products of 8-bit operands with
  * both scales, fp32 sums, the bias (fp32 [N], or NULL) added in fp32, one
- * rounding to dtype.  workspace: moeca_quant_linear_bytes(M, K) bytes, 256-byte
+ * rounding to dtype.  For bf16 results the matrix instructions may align the
+ * products of eight consecutive k to the largest of them and keep 2^-13 of it
+ * (1.5e-5 of a row's 2-norm on normal values, where the rounding is 4e-3); fp32
+ * results have exact products.  workspace: moeca_quant_linear_bytes(M, K) bytes, 256-byte
  * aligned, for the quantised rows; calls that overlap in time need one each.
  * M = 0 does nothing.  A row's sums do not depend on the other rows of the
  * call, except that M may choose another order of the sums over K. */

@@ -352,8 +352,8 @@ __device__ __forceinline__ void mfma_q8(const Piece<true>& w, const Piece<true>&
 // Persistent, one block per CU; the next tile's first loads start before this
 // tile's epilogue.  Measured, 64 experts of 2048 x 1408, 4 x 1024 tokens, eight
 // branches each: 256 us with the quantising of x, 1.48 PFLOP/s (EXACT 451 us, 0.84
-// PFLOP/s: the conversions fill the memory slot).  Two blocks of 64 x 256 a CU do not
-// fit its LDS, and one took longer than this from some 50 rows an expert on.
+// PFLOP/s: the conversions fill the memory slot).  For few rows an
+// expert the kernel below has tiles of 64 x 256 (q8_plan).
 // ---------------------------------------------------------------------------
 constexpr int kMidTM = 128;
 constexpr int kMidTN = 256;
@@ -1441,7 +1441,10 @@ FfnPlan q8_plan(const Shape& s, int64_t rows) {
   p.tm = q8_tile(tiles(s.d), kd, !s.bf16, s.bf16 && tall_capable(s.mid_rows(), s.d_ff), 64);
   p.tall_up = p.tm_up == kTallTM;
   p.tall_down = p.tm == kTallTM;
-  // gated: 64-row tiles, one block per CU, for few rows only
+  // Gated: 64-row tiles, one block per CU, where most experts have one.  Up, us, 64
+  // against 128 rows, 64 experts of 2048 x 1408 with 18, 36 and 72 rows (an eighth above
+  // the mean), EXACT: 75 84, 85 86, 124 105; not EXACT, 36 and 72: 74 76, 97 80.  (16
+  // of 1152 x 2304 with 72 would rather have 64: 37 46, 29 33.)
   if (s.swiglu && !p.tall_up) p.tm_up = mean <= 48 ? 64 : kMidTM;
   p.tn_up = p.tall_up || s.swiglu ? 256 : 128;
   p.tn_down = p.tall_down ? kTallTN : 128;

@@ -126,18 +126,20 @@ class MoecaLayer:
     def bind_attention(self, attn_in, attn_cache):
         """``attn_cache``: a tensor like ``attn_in``, or, for cache="e4m3", a
         ``quant.QuantRows`` of B*N rows of width d."""
-        if self.cache8 and attn_cache is not None:
-            if ((attn_cache.slots, attn_cache.K) != (self.B * self.N, self.d) or
+        from . import quant
+        if isinstance(attn_cache, quant.QuantRows) != (self.cache8 and attn_cache is not None):
+            raise TypeError("a cache='e4m3' layer takes quant.QuantRows, others a tensor")
+        if self.cache8:
+            if attn_cache is not None and (
+                    (attn_cache.slots, attn_cache.K) != (self.B * self.N, self.d) or
                     attn_cache.q.device != self.device):
                 raise ValueError(f"expected {self.B * self.N} quantised rows of width {self.d} "
                                  f"on {self.device}")
-            _lib.moeca_bind_attention_quant(self.h, attn_in.data_ptr(), attn_cache.q.data_ptr(),
-                                            attn_cache.scale.data_ptr())
+            _lib.moeca_bind_attention_quant(
+                self.h, None if attn_in is None else attn_in.data_ptr(),
+                None if attn_cache is None else attn_cache.q.data_ptr(),
+                None if attn_cache is None else attn_cache.scale.data_ptr())
             self._attn = (attn_in, attn_cache)
-            return
-        if self.cache8:
-            _lib.moeca_bind_attention_quant(self.h, None, None, None)
-            self._attn = None
             return
         self._attn = (attn_in, attn_cache)
         _lib.moeca_bind_attention(self.h, None if attn_in is None else attn_in.data_ptr(),
@@ -163,6 +165,8 @@ class MoecaLayer:
         B*N*k rows (slot q of token i at row i*k + q): a view of the workspace."""
         from . import quant
         torch = _torch()
+        if not self.cache8:
+            raise ValueError("the layer's cache is not quantised")
         n = self.B * self.N * self.k
         return quant.QuantRows(n, self.d, q=self.buffer("h_c").view(n, -1),
                                scale=self.buffer("s_c").view(n, -1),

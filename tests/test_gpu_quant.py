@@ -669,3 +669,63 @@ def test_layer_tiles(i):
     for t in range(3):
         c.step(t, form)
         c.drift(0.02 if t == 0 else 0.6)
+
+
+def test_python_refusals_and_streams():
+    """What the wrappers refuse before a launch; products on a stream of their own."""
+    import torch
+    from paper_2606_15615_amd import quant
+    c = Case(128, 4, 2, 128, 1, 40, seed=1)
+    plain = Case(128, 4, 2, 128, 1, 40, seed=1, cache=False)
+    with pytest.raises(TypeError):
+        c.L.bind_attention(c.attn_in, torch.zeros_like(c.attn_in))
+    with pytest.raises(TypeError):
+        plain.L.bind_attention(c.attn_in, c.attn)
+    with pytest.raises(ValueError):
+        c.L.bind_attention(c.attn_in, quant.QuantRows(39, 128))
+    for args in ((c.attn_in, None), (None, c.attn)):
+        with pytest.raises(Exception, match="NULL"):
+            c.L.bind_attention(*args)
+    with pytest.raises(ValueError):
+        plain.L.cache_rows()
+    c.L.bind_attention(None, None)
+    c.attn = None
+    c.step(0, "unbound")
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(2)
+    W = quant.quantize_matrix(torch.randn(300, 500, generator=g, device="cuda:0"))
+    side = torch.cuda.Stream()
+    for M in (5, 70):
+        xs = [torch.randn(M, 500, generator=g, device="cuda:0").bfloat16() for _ in range(2)]
+        want = [quant.linear(x, W) for x in xs]
+        with pytest.raises(ValueError):
+            quant.linear(xs[0], W, stream=side)
+        # two at a time, a workspace each
+        ws = [quant.linear_workspace(M, 500) for _ in range(2)]
+        out = [torch.zeros_like(w) for w in want]
+        torch.cuda.synchronize()
+        for _ in range(20):
+            quant.linear(xs[0], W, out=out[0], workspace=ws[0])
+            quant.linear(xs[1], W, out=out[1], workspace=ws[1], stream=side)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("d", [1984, 2112])
+def test_wide_rows(d):
+    """Rows of four groups of 512 elements, and of more."""
+    c = Case(d, 4, 2, 64, 1, 60, mode="threshold", tau0=0.8, seed=d)
+    for t in range(3):
+        c.step(t, f"d {d}")
+        c.drift(0.2)
+
+
+def test_routing_to_one_expert():
+    """Every token takes the same expert, the others have none."""
+    import torch
+    for act, B, N in (("gelu_tanh", 2, 900), ("swiglu", 1, 300)):
+        c = Case(256, 8, 1, 192, B, N, act=act, mode="threshold", tau0=8.0, seed=6)
+        c.x[:, :] = np.abs(c.x[:1]) + 0.01 * c.g.normal(size=c.x.shape)
+        c.step(0, "one row of tokens")
+        c.drift(0.001)
+        c.step(1, "again")
