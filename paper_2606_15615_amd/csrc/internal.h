@@ -215,9 +215,10 @@ hipError_t launch_dequant_rows(const uint8_t* q, const uint8_t* s, int64_t slots
                                int64_t ld, hipStream_t st);
 hipError_t launch_quant_matrix(const void* W, bool bf16, int count, int N, int K, uint8_t* q,
                                uint8_t* s, hipStream_t st);
-// The combine of a cache8 layer: recomputed rows from b.fresh into the cache.
+// The combine of a cache8 layer: recomputed rows from b.fresh into the cache.  full:
+// a step that recomputes every branch.
 hipError_t launch_combine_q8(const Shape& s, void* out, const void* attn_in, uint8_t* attn_q,
-                             uint8_t* attn_s, const Buffers& b, hipStream_t st);
+                             uint8_t* attn_s, bool full, const Buffers& b, hipStream_t st);
 // rows: branches the routed experts are expected to have in this step
 FfnPlan q8_plan(const Shape& s, int64_t rows);
 hipError_t launch_q8_up(const Shape& s, int act, const FfnPlan& plan, const QuantWeights& w,

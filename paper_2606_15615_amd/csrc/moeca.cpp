@@ -209,7 +209,9 @@ hipError_t ffn_up(const moeca_layer* L, const Shape& s, const void* x, const moe
                                                 nullptr, st);
   if (e != hipSuccess) return e;
   moeca::launch_events() = {nullptr, ev.stop};
-  return moeca::launch_q8_up(s, L->pol.act, plan, L->qw, b, st);
+  const hipError_t u = moeca::launch_q8_up(s, L->pol.act, plan, L->qw, b, st);
+  if (u != hipSuccess) moeca::launch_events() = {};
+  return u;
 }
 
 hipError_t ffn_down(const moeca_layer* L, const Shape& s, const moeca::FfnPlan& plan,
@@ -620,7 +622,8 @@ int layer_step(moeca_layer* L, const void* x_t, const void* x_ffn, int t, void* 
   if (!check(ffn_down(L, s, plan, b, st), "ffn down"))
     return MOECA_E_HIP;
   arm();
-  if (!check(s.cache8 ? moeca::launch_combine_q8(s, out, L->attn_in, L->attn_q, L->attn_s, b, st)
+  if (!check(s.cache8 ? moeca::launch_combine_q8(s, out, L->attn_in, L->attn_q, L->attn_s, full, b,
+                                                  st)
                       : moeca::launch_combine(s, uncached ? 0 : 1,
                                               moeca::combine_sums(s) ? plan.split_down : 1, out,
                                               L->attn_in, L->attn_cache, b, st),

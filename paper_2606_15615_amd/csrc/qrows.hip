@@ -146,12 +146,14 @@ __global__ __launch_bounds__(256) void quant_matrix_kernel(const T* __restrict__
 // what is stored; a synchronised token's attention feature goes into its row of
 // the 8-bit attention cache.
 // ---------------------------------------------------------------------------
-// One wave per token.  Where the row is loaded from depends on the branch, so a
-// token costs two round trips: what the decision left, then every row's elements
-// (GI groups of 512 a lane's eight of each; GI = 0: any width, a group at a time),
-// all asked for before any is used.  8192 tokens of 1152, two branches: a full step
-// 32 us (104 MB), a cache step 17.5 us, of five waves a SIMD; six (80 registers) 1.4 us
-// more, eight (64, spilled) 12 us more.
+// One wave per token.  Where a row is loaded from depends on the branch: a recomputed
+// one costs two round trips, what the decision left, then the row's elements (GI
+// groups of 512 a lane's eight of each; GI = 0: any width, a group at a time), all
+// asked for before any is used.  The token's own slots need no decision: with GI > 0
+// (two of them at most) they are asked for first, `reuse` (a step that may reuse
+// some).  8192 tokens of 1152, two branches: a full step 32 us (104 MB), with three
+// cache steps 18.3 us on average (20.4 with the slots after the decision, and then
+// 21.7 and 32.5 in registers for six and eight waves a SIMD).
 template <typename T> struct Raw;  // eight elements as loaded; 8-bit rows use the first two words
 template <> struct Raw<uint16_t> {
   typedef __attribute__((ext_vector_type(4))) unsigned int v;
@@ -180,7 +182,7 @@ __global__ __launch_bounds__(kRowWaves * kWave) void combine_q8_kernel(
     int32_t* __restrict__ e_c, float* __restrict__ w_c, float* __restrict__ n_c,
     T* __restrict__ out, const T* __restrict__ attn_in, uint8_t* __restrict__ attn_q,
     uint8_t* __restrict__ attn_s, const T* __restrict__ h_sh, int S, int64_t T_tokens, int d,
-    int k) {
+    int k, int reuse) {
   typedef typename Raw<T>::v raw;
   const int lane = threadIdx.x & (kWave - 1);
   const int64_t t = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x)) *
@@ -188,6 +190,10 @@ __global__ __launch_bounds__(kRowWaves * kWave) void combine_q8_kernel(
                     __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
   if (t >= T_tokens) return;
   const int pitch = static_cast<int>(q8_pitch(d)), spitch = static_cast<int>(q8_spitch(d));
+  static_assert(GI == 0 || KMAX == 2, "a slot is one of two");
+  constexpr int G = GI > 0 ? GI : 1;
+  uint2 own[KMAX][G];  // the token's slots
+  int own_s[KMAX][G];
   float wp[KMAX];
   int slot[KMAX], from[KMAX];  // from: row of `fresh`, -1 for a reused branch
   double ss[KMAX];
@@ -202,14 +208,33 @@ __global__ __launch_bounds__(kRowWaves * kWave) void combine_q8_kernel(
       wp[p] = w_t[f];
       slot[p] = sigma[f];
       const int at = pos[f];
-      // the same for the whole wave: say so, so that branches on it are scalar
-      from[p] = __builtin_amdgcn_readfirstlane(mask[f] != 0 ? at : -1);
+      from[p] = mask[f] != 0 ? at : -1;
     }
   }
-  const bool syn =
-      __builtin_amdgcn_readfirstlane(attn_in != nullptr && sync[t] != 0 ? 1 : 0) != 0;
+  int syn_v = 0;
+  if (attn_in != nullptr) syn_v = sync[t];
+  if constexpr (GI > 0) {
+#pragma unroll
+    for (int p = 0; p < KMAX; ++p)
+#pragma unroll
+      for (int gi = 0; gi < G; ++gi) {
+        own[p][gi] = make_uint2(0, 0);
+        own_s[p][gi] = 0;
+        const int c = (gi * kWave + lane) * 8;
+        if (reuse != 0 && p < k && c < d) {
+          own[p][gi] = *reinterpret_cast<const uint2*>(h_c + (t * k + p) * pitch + c);
+          own_s[p][gi] = s_c[(t * k + p) * spitch + c / kBlk];
+        }
+      }
+  }
+  // the same for the whole wave: say so, so that branches on it are scalar
+#pragma unroll
+  for (int p = 0; p < KMAX; ++p) {
+    from[p] = __builtin_amdgcn_readfirstlane(from[p]);
+    slot[p] = __builtin_amdgcn_readfirstlane(slot[p]);
+  }
+  const bool syn = __builtin_amdgcn_readfirstlane(syn_v) != 0;
 
-  constexpr int G = GI > 0 ? GI : 1;
   for (int base = 0; base < (GI > 0 ? 1 : pitch); base += 8 * kWave) {
     raw h[KMAX][G], a[G];
     int sb[KMAX][G];
@@ -225,6 +250,11 @@ __global__ __launch_bounds__(kRowWaves * kWave) void combine_q8_kernel(
         if (from[p] >= 0) {  // uniform across the wave
           h[p][gi] = __builtin_nontemporal_load(
               reinterpret_cast<const raw*>(fresh + int64_t(from[p]) * d + c));
+        } else if constexpr (GI > 0) {
+          const uint2 q = slot[p] == 0 ? own[0][gi] : own[1][gi];
+          h[p][gi][0] = q.x;
+          h[p][gi][1] = q.y;
+          sb[p][gi] = slot[p] == 0 ? own_s[0][gi] : own_s[1][gi];
         } else {
           const int64_t r = t * k + slot[p];
           const uint2 q = *reinterpret_cast<const uint2*>(h_c + r * pitch + c);
@@ -361,14 +391,15 @@ hipError_t launch_quant_matrix(const void* W, bool bf16, int count, int N, int K
 }
 
 hipError_t launch_combine_q8(const Shape& s, void* out, const void* attn_in, uint8_t* attn_q,
-                             uint8_t* attn_s, const Buffers& b, hipStream_t st) {
+                             uint8_t* attn_s, bool full, const Buffers& b, hipStream_t st) {
   const dim3 grid(static_cast<unsigned>((s.tokens() + kRowWaves - 1) / kRowWaves));
   const dim3 block(kRowWaves * kWave);
 #define MOECA_CQ8(T, KM, GI)                                                                     \
   launch_kernel(&combine_q8_kernel<T, KM, GI>, grid, block, 0, st, b.w_t, b.e_t, b.sigma, b.mask, \
                 b.sync, b.pos, static_cast<const T*>(b.fresh), static_cast<uint8_t*>(b.h_c),     \
                 b.s_c, b.e_c, b.w_c, b.n_c, static_cast<T*>(out), static_cast<const T*>(attn_in), \
-                attn_q, attn_s, static_cast<const T*>(b.h_sh), s.S, s.tokens(), s.d, s.k)
+                attn_q, attn_s, static_cast<const T*>(b.h_sh), s.S, s.tokens(), s.d, s.k,     \
+                full ? 0 : 1)
   const int64_t gi = (q8_pitch(s.d) + 8 * kWave - 1) / (8 * kWave);
   if (s.bf16 && s.k <= 2 && gi <= 2) MOECA_CQ8(uint16_t, 2, 2);
   else if (s.bf16 && s.k <= 2 && gi <= 3) MOECA_CQ8(uint16_t, 2, 3);
