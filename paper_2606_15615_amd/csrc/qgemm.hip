@@ -599,7 +599,8 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_gated_kernel(QArgs a) {
 // instructions); with few, the stream of the weights (256 tokens of the same layer: up
 // 85 MB in 21 to 25 us, 576 tiles for 512 places; down 20.5 us, 4.1 TB/s).  A ring of
 // six k-tiles instead of three left down at 21 and slowed up to 33 us (one block per
-// CU).  Dense 333 x 1152 x 4608 10.9 us, 1000 rows 17.6 us.
+// CU).  Four stages of half a k-tile, three ahead, in the LDS of the two stages of
+// 128 EXACT rows took 7 % longer.  Dense 333 x 1152 x 4608 10.9 us, 1000 rows 17.6 us.
 // ---------------------------------------------------------------------------
 template <int TM, bool GATED> struct Duo {
   static constexpr int TN = GATED ? 256 : 128;
