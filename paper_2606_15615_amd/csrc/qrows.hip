@@ -151,9 +151,9 @@ __global__ __launch_bounds__(256) void quant_matrix_kernel(const T* __restrict__
 // groups of 512 a lane's eight of each; GI = 0: any width, a group at a time), all
 // asked for before any is used.  The token's own slots need no decision: with GI > 0
 // (two of them at most) they are asked for first, `reuse` (a step that may reuse
-// some).  8192 tokens of 1152, two branches: a full step 28 us (104 MB), a
-// cache step 16.5 us, 18.3 us on average over a cycle (20.4 with the slots after the decision, and then
-// 21.7 and 32.5 in registers for six and eight waves a SIMD).
+// some).  8192 tokens of 1152, two branches: a full step 28 us (104 MB), a cache step
+// 16.5 us, 18.3 us on average over a cycle (20.4 with the slots after the decision, and
+// then 21.7 and 32.5 in registers for six and eight waves a SIMD).
 template <typename T> struct Raw;  // eight elements as loaded; 8-bit rows use the first two words
 template <> struct Raw<uint16_t> {
   typedef __attribute__((ext_vector_type(4))) unsigned int v;
