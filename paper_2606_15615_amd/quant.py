@@ -165,7 +165,8 @@ def quantize_matrix(W, stream=None) -> QuantMatrix:
     N, K = W.shape[-2:]
     lead = tuple(W.shape[:-2])
     q = torch.empty(lead + (N, _lib.moeca_quant_pitch(K)), dtype=torch.uint8, device=W.device)
-    s = torch.zeros(lead + (-(-N // 128), _lib.moeca_quant_scale_pitch(K)), dtype=torch.uint8,
+    # no fill: nothing orders one on the current stream against the kernel on `stream`
+    s = torch.empty(lead + (-(-N // 128), _lib.moeca_quant_scale_pitch(K)), dtype=torch.uint8,
                     device=W.device)
     _launch(_lib.load().moeca_quant_matrix, W.device, stream, W.data_ptr(), _dtype(W),
             lead[0] if lead else 1, N, K, q.data_ptr(), s.data_ptr())

@@ -1,0 +1,38 @@
+"""On which stream the 8-bit wrappers allocate and launch: host checks, nothing runs
+on a GPU.  Launches and allocations are recorded in place of being made."""
+import pytest
+
+
+class Stream:
+    """What a call asks a stream for."""
+
+    def __init__(self, index=0):
+        import torch
+        self.device = torch.device("cuda", index)
+        self.cuda_stream = 0x5000 + index
+
+
+@pytest.fixture
+def quant(monkeypatch):
+    """The module with launches recorded: (device, stream, arguments)."""
+    from paper_2606_15615_amd import quant as m
+    m.launches = []
+    monkeypatch.setattr(m, "_launch",
+                        lambda fn, device, stream, *a: m.launches.append((device, stream, a)))
+    yield m
+    del m.launches
+
+
+def test_scales_of_a_matrix_are_not_filled(quant, monkeypatch):
+    """A fill would run on the current stream and the kernel that writes the scales on
+    the call's, in no order."""
+    import torch
+
+    def no_fill(*a, **k):
+        raise AssertionError("a fill on the current stream")
+    for name in ("zeros", "full", "ones"):
+        monkeypatch.setattr(torch, name, no_fill)
+    for shape in ((70, 200), (3, 130, 260)):
+        m = quant.quantize_matrix(torch.empty(shape), stream=Stream())
+        assert m.q.shape[:-2] == shape[:-2] and (m.N, m.K) == shape[-2:]
+    assert len(quant.launches) == 2
