@@ -6,7 +6,7 @@ read back by slot; ``QuantMatrix`` holds one weight matrix, or a stack of them,
 with a scale per 128 x 128 block; ``linear`` multiplies rows with a matrix.
 torch provides device memory and the stream; the arithmetic runs in the
 library's kernels.  Calls run on their tensors' device, on its current stream
-unless one is given.
+unless one is given, to which a tensor that such a call makes then belongs.
 """
 from __future__ import annotations
 
@@ -40,6 +40,15 @@ def _launch(fn, device, stream, *args):
             rc = fn(*args, raw)
     if rc != _lib.MOECA_OK:
         _lib._check(rc)
+
+
+def _empty(shape, dtype, device, stream):
+    """A new tensor that belongs to the call's stream: one of the current stream could
+    still be in use there when a call on another writes it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _rows(t, width, device, what):
@@ -127,7 +136,7 @@ class QuantRows:
         at = _indexes(slot, None, self.device)
         rows = self.slots if slot is None else slot.shape[0]
         if out is None:
-            out = torch.empty(rows, self.K, dtype=dtype or _BF16, device=self.device)
+            out = _empty((rows, self.K), dtype or _BF16, self.device, stream)
         elif dtype is not None and out.dtype != dtype:
             raise TypeError(f"out is {out.dtype}, not {dtype}")
         p, n, ld = _rows(out, self.K, self.device, "out")
@@ -164,10 +173,9 @@ def quantize_matrix(W, stream=None) -> QuantMatrix:
         raise ValueError("W is a contiguous [N][K] or [n][N][K] tensor")
     N, K = W.shape[-2:]
     lead = tuple(W.shape[:-2])
-    q = torch.empty(lead + (N, _lib.moeca_quant_pitch(K)), dtype=torch.uint8, device=W.device)
-    # no fill: nothing orders one on the current stream against the kernel on `stream`
-    s = torch.empty(lead + (-(-N // 128), _lib.moeca_quant_scale_pitch(K)), dtype=torch.uint8,
-                    device=W.device)
+    q = _empty(lead + (N, _lib.moeca_quant_pitch(K)), torch.uint8, W.device, stream)
+    s = _empty(lead + (-(-N // 128), _lib.moeca_quant_scale_pitch(K)), torch.uint8, W.device,
+               stream)
     _launch(_lib.load().moeca_quant_matrix, W.device, stream, W.data_ptr(), _dtype(W),
             lead[0] if lead else 1, N, K, q.data_ptr(), s.data_ptr())
     return QuantMatrix(q, s, N, K)
@@ -189,7 +197,7 @@ def linear(x, W: QuantMatrix, bias=None, out=None, workspace=None, stream=None):
     px, M, ldx = _rows(x, W.K, device, "x")
     dt = _dtype(x)
     if out is None:
-        out = torch.empty(M, W.N, dtype=x.dtype, device=device)
+        out = _empty((M, W.N), x.dtype, device, stream)
     elif out.dtype != x.dtype:
         raise TypeError(f"out is {out.dtype}, x {x.dtype}")
     po, n, ldo = _rows(out, W.N, device, "out")

@@ -48,3 +48,32 @@ def test_matrix_on_another_stream(shape):
         torch.cuda.synchronize()
         assert torch.equal(got.q, want.q)
         assert torch.equal(got.scale[..., :nb], want.scale[..., :nb])
+
+
+def test_results_on_another_stream():
+    """Results that a call on a side stream makes are not memory that the busy current
+    stream still uses: blocks it has just given back keep their last readers."""
+    import torch
+    from paper_2606_15615_amd import quant
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(4)
+    x = torch.randn(500, 640, generator=g, device="cuda:0").bfloat16()
+    W = quant.quantize_matrix(torch.randn(384, 640, generator=g, device="cuda:0"))
+    ws = quant.linear_workspace(500, 640)
+    rows = quant.QuantRows(500, 640)
+    rows.write(x)
+    big = torch.randn(2048, 2048, generator=g, device="cuda:0") / 45
+    want = quant.linear(x, W), rows.read()
+    side = torch.cuda.Stream()
+    for call, ref in ((lambda: quant.linear(x, W, workspace=ws, stream=side), want[0]),
+                      (lambda: rows.read(stream=side), want[1])):
+        for _ in range(3):
+            torch.cuda.synchronize()
+            _busy(big)
+            old = torch.full_like(ref, 3.0)      # late, on the current stream
+            seen = old + 1
+            del old
+            got = call()
+            torch.cuda.synchronize()
+            assert torch.equal(got, ref) and bool((seen == 4.0).all())
+            del got, seen

@@ -36,3 +36,37 @@ def test_scales_of_a_matrix_are_not_filled(quant, monkeypatch):
         m = quant.quantize_matrix(torch.empty(shape), stream=Stream())
         assert m.q.shape[:-2] == shape[:-2] and (m.N, m.K) == shape[-2:]
     assert len(quant.launches) == 2
+
+
+def test_new_tensors_belong_to_the_calls_stream(quant, monkeypatch):
+    import torch
+    now, made, empty = [None], [], torch.empty
+
+    class on:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            now[0] = self.stream
+
+        def __exit__(self, *a):
+            now[0] = None
+
+    def recorded(*a, **k):
+        made.append(now[0])
+        return empty(*a, **k)
+
+    r = quant.QuantRows(6, 200, device="cpu")
+    W = quant.quantize_matrix(torch.empty(70, 200))
+    ws = quant.linear_workspace(5, 200, "cpu")
+    x, out = torch.empty(5, 200), torch.empty(5, 70)
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch, "empty", recorded)
+    s = Stream()
+    for call, n in ((lambda **k: r.read(**k), 1), (lambda **k: quant.quantize_matrix(x, **k), 2),
+                    (lambda **k: quant.linear(x, W, workspace=ws, **k), 1),
+                    (lambda **k: quant.linear(x, W, out=out, workspace=ws, **k), 0)):
+        for stream in (None, s):
+            made.clear()
+            call(stream=stream)
+            assert made == [stream] * n and quant.launches[-1][1] is stream
