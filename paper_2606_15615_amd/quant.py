@@ -32,6 +32,8 @@ def _launch(fn, device, stream, *args):
     index = device.index
     if index is None or device.type != "cuda":
         raise ValueError(f"the tensors are on {device}, not on a GPU")
+    if stream is not None and stream.device != device:
+        raise ValueError(f"the stream is one of {stream.device}, the tensors are on {device}")
     raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
     if torch.cuda.current_device() == index:
         rc = fn(*args, raw)

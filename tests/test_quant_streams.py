@@ -70,3 +70,13 @@ def test_new_tensors_belong_to_the_calls_stream(quant, monkeypatch):
             made.clear()
             call(stream=stream)
             assert made == [stream] * n and quant.launches[-1][1] is stream
+
+
+def test_a_stream_of_another_device_is_refused():
+    import torch
+    from paper_2606_15615_amd import quant
+
+    def never(*a):
+        raise AssertionError("launched")
+    with pytest.raises(ValueError, match="stream is one of cuda:1"):
+        quant._launch(never, torch.device("cuda", 0), Stream(1))
