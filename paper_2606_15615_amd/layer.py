@@ -59,7 +59,6 @@ class MoecaLayer:
         self.n_shared = n_shared
         self.dtype = dtype
         self.act_np = np.uint16 if dtype == "bf16" else np.float32
-        self.device = torch.device(device)
         self.up_rows = d_ff * (2 if act == "swiglu" else 1)
         self.experts8, self.cache8 = experts is not None, cache is not None
         self.h = _lib.moeca_layer_create(d, E, k, d_ff, p)
@@ -67,7 +66,8 @@ class MoecaLayer:
             _lib.moeca_layer_set_quant(self.h, (_lib.MOECA_QUANT_EXPERTS if self.experts8 else 0) |
                                        (_lib.MOECA_QUANT_CACHE if self.cache8 else 0))
         nbytes = _lib.moeca_workspace_bytes(self.h)
-        self._ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        self._ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
+        self.device = self._ws.device  # with its index: "cuda" is the one current by now
         base = self._ws.data_ptr()
         self._ws_shift = (-base) % 256
         self.workspace = self._ws[self._ws_shift:self._ws_shift + nbytes]

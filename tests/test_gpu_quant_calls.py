@@ -77,3 +77,44 @@ def test_results_on_another_stream():
             torch.cuda.synchronize()
             assert torch.equal(got, ref) and bool((seen == 4.0).all())
             del got, seen
+
+
+def _layer(d, E, k, d_ff, B, N, seed=0, dtype="bf16", bias=False, **kw):
+    """A layer with random weights, 8-bit where it is asked for, and its input."""
+    import torch
+    from paper_2606_15615_amd import quant
+    from paper_2606_15615_amd.layer import MoecaLayer
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(seed)
+
+    def rnd(*s):
+        t = torch.randn(*s, generator=g, device="cuda:0")
+        return t.bfloat16() if dtype == "bf16" else t
+    L = MoecaLayer(d, E, k, d_ff, batch=B, tokens=N, dtype=dtype, **kw)
+    U = L.up_rows
+    w = [rnd(E, U, d) / d ** 0.5, rnd(E, d, d_ff) / d_ff ** 0.5]
+    put = L.set_weights
+    if L.experts8:
+        w, put = [quant.quantize_matrix(m) for m in w], L.set_weights_quant
+    put(rnd(E, d) / d ** 0.5, None, *w)
+    if L.n_shared:
+        s = [rnd(L.n_shared, U, d) / d ** 0.5, rnd(L.n_shared, d, d_ff) / d_ff ** 0.5]
+        (L.set_shared_quant(*map(quant.quantize_matrix, s)) if L.experts8 else L.set_shared(*s))
+    L.reset()
+    return L, rnd(B, N, d)
+
+
+def test_a_device_without_an_index():
+    """"cuda" is the current device: the same results as on "cuda:0"."""
+    import torch
+    from paper_2606_15615_amd import quant
+    ys = []
+    for device in ("cuda:0", "cuda"):
+        L, x = _layer(192, 4, 2, 128, 1, 50, device=device, experts="e4m3", cache="e4m3")
+        att = quant.QuantRows(50, 192, device=device)
+        L.bind_attention(x, att)
+        y = torch.zeros_like(x)
+        L.step(x, 0, y)
+        ys.append((y, att.q))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*ys))
