@@ -351,6 +351,7 @@ int moeca_layer_set_quant(moeca_layer* L, int flags) {
   }
   L->shape.experts8 = experts;
   L->shape.cache8 = cache;
+  L->shape.exact_hidden = cache;
   L->layout = make_layout(L->shape);
   L->ws = nullptr;  // the layout changed: bind again
   L->valid = false;
@@ -452,7 +453,7 @@ int moeca_forward_noalloc(const moeca_layer* L, const void* x, int samples, void
     return fail(MOECA_E_INVAL, "samples must be in [1, " + std::to_string(L->shape.B) + "]");
   Shape s = L->shape;
   s.B = samples;
-  s.cache8 = false;  // no cache here, quantised or not
+  s.cache8 = false;  // no cache here, quantised or not; its layer's products stay exact
   // with the down projection's K pieces if they fit (fp32 layers, and bf16
   // calls of few enough rows for the weight-streaming tiles)
   const bool split = !s.bf16 || s.branches() <= int64_t(moeca::kThinRows) * s.E;

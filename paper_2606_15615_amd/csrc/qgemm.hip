@@ -1375,7 +1375,7 @@ bool tall_capable(int64_t rows, int K) {
 }
 
 // Whether the up projection takes the exact products (above).
-bool exact_up(const Shape& s) { return !s.bf16 || s.cache8; }
+bool exact_up(const Shape& s) { return !s.bf16 || s.exact_hidden; }
 
 // The tile height (32, 64, 128, or 256 for the 256-column tiles) that takes least
 // time: blocks come in rounds of two per CU, the last one perhaps of one, which is

@@ -118,3 +118,24 @@ def test_a_device_without_an_index():
         ys.append((y, att.q))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(*ys))
+
+
+@pytest.mark.parametrize("kw", [
+    dict(d=256, E=8, k=2, d_ff=448, B=2, N=120),
+    dict(d=192, E=4, k=3, d_ff=320, B=1, N=90, act="swiglu", n_shared=1),
+    dict(d=640, E=4, k=2, d_ff=1088, B=1, N=900)])
+@pytest.mark.parametrize("cache", [None, "e4m3"])
+def test_noalloc_is_the_full_step(kw, cache):
+    """moeca_forward_noalloc computes what a full step does, with the products that the
+    layer's hidden rows take (exact ones where its cache is in 8 bits)."""
+    import torch
+    from paper_2606_15615_amd import _lib
+    say(f"  {kw} cache {cache}")
+    L, x = _layer(**kw, seed=5, experts="e4m3", cache=cache)
+    y, z = torch.zeros_like(x), torch.zeros_like(x)
+    L.step(x, 0, y)
+    _lib.moeca_forward_noalloc(L.h, x.data_ptr(), L.B, z.data_ptr(),
+                               torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert L.stats().full_step == 1
+    assert torch.equal(y, z)
