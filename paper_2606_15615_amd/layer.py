@@ -125,7 +125,7 @@ class MoecaLayer:
 
     def bind_attention(self, attn_in, attn_cache):
         """``attn_cache``: a tensor like ``attn_in``, or, for cache="e4m3", a
-        ``quant.QuantRows`` of B*N rows of width d."""
+        ``quant.QuantRows`` of B*N rows of width d without norms."""
         from . import quant
         if isinstance(attn_cache, quant.QuantRows) != (self.cache8 and attn_cache is not None):
             raise TypeError("a cache='e4m3' layer takes quant.QuantRows, others a tensor")
@@ -135,6 +135,9 @@ class MoecaLayer:
                     attn_cache.q.device != self.device):
                 raise ValueError(f"expected {self.B * self.N} quantised rows of width {self.d} "
                                  f"on {self.device}")
+            if attn_cache is not None and attn_cache.norm is not None:
+                raise ValueError("a step writes the rows' elements and scales, not their norms: "
+                                 "bind QuantRows without a norm")
             _lib.moeca_bind_attention_quant(
                 self.h, None if attn_in is None else attn_in.data_ptr(),
                 None if attn_cache is None else attn_cache.q.data_ptr(),

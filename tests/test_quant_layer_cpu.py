@@ -53,3 +53,12 @@ def test_the_layers_device_is_its_workspaces(layer, device):
     L.bind_attention(w, _rows(8, 128))
     with pytest.raises(ValueError, match="expected 4 quantised matrices"):
         L.set_weights_quant(w, None, _stack(4, 64, 64), _stack(4, 128, 64))
+
+
+def test_an_attention_cache_with_norms_is_refused(layer):
+    """A step would leave its norms those of rows that are gone."""
+    L = layer(cache="e4m3")
+    x = _bytes(8, 128 * 2)
+    with pytest.raises(ValueError, match="without a norm"):
+        L.bind_attention(x, _rows(8, 128, norm=True))
+    L.bind_attention(x, _rows(8, 128))
