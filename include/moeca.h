@@ -134,9 +134,10 @@ int moeca_layer_set_shared(moeca_layer* layer, const void* W_up_s, const void* W
  *   MOECA_QUANT_EXPERTS  the step quantises its FFN input, multiplies 8-bit
  *     operands, and quantises each expert's hidden rows act(W_up x) from their
  *     fp32 values; the down projection's rows are of the policy dtype as
- *     before.  Products are those of moeca_quant_linear() in the policy dtype, but
- *     exact for the hidden rows of layers with MOECA_QUANT_CACHE.  Shared experts are held the same way, the router is not.  The
- *     weights are bound with moeca_layer_set_weights_quant() (and
+ *     before.  Products are those of moeca_quant_linear() in the policy dtype
+ *     for more than 16 rows, but exact, as for fp32, in layers with
+ *     MOECA_QUANT_CACHE.  Shared experts are held the same way, the router is
+ *     not.  The weights are bound with moeca_layer_set_weights_quant() (and
  *     moeca_layer_set_shared_quant()) in the place of the plain calls.
  *   MOECA_QUANT_CACHE    cached branch rows are 8-bit, their norms those of the
  *     stored values; a step's output takes a recomputed branch's row as the

@@ -60,8 +60,8 @@ struct Shape {
   bool erf = false;     // erf GELU
   bool experts8 = false;  // expert weights and hidden rows in 8 bits (q8.h)
   bool cache8 = false;    // cache rows in 8 bits
-  bool exact_hidden = false;  // experts8: hidden rows from exact products (a layer with an
-                              // 8-bit cache, also in calls that have no cache)
+  bool exact8 = false;    // experts8: exact products (a layer with an 8-bit cache, also in
+                          // calls that have no cache)
   int64_t tokens() const { return int64_t(B) * N; }
   int64_t branches() const { return int64_t(B) * N * k; }
   size_t act_bytes() const { return bf16 ? 2 : 4; }

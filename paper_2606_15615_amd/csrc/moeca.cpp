@@ -351,7 +351,7 @@ int moeca_layer_set_quant(moeca_layer* L, int flags) {
   }
   L->shape.experts8 = experts;
   L->shape.cache8 = cache;
-  L->shape.exact_hidden = cache;
+  L->shape.exact8 = cache;
   L->layout = make_layout(L->shape);
   L->ws = nullptr;  // the layout changed: bind again
   L->valid = false;

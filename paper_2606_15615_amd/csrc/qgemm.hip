@@ -18,11 +18,14 @@
 // show, EXACT converts the operands in registers to bf16, which holds every
 // e4m3 number and power of two, and takes the bf16 instructions with fp32 sums:
 //  - fp32 results;
-//  - hidden rows of a layer whose cache is 8-bit too: a hidden element that
-//    moves over a rounding border (1 in 200 does, at 1.5e-5) moves the down
-//    projection's row by 1.4e-3, and 1.6 % of the cached elements by a whole
-//    step of 2^-3: reused branches were 5.7e-3 off the 64-bit definition
-//    instead of 1.7e-3.
+//  - both products of a layer whose cache is 8-bit too, since what is cached is
+//    rounded to 8 bits once more.  Up: a hidden element that moves over a rounding
+//    border (1 in 200 does, at 1.5e-5) moves the down projection's row by 1.4e-3,
+//    and 1.6 % of the cached elements by a whole step of 2^-3: reused branches were
+//    5.7e-3 off the 64-bit definition instead of 1.7e-3.  Down: one or two cached
+//    elements in 10^4 moved by a step, and one scale in 10^5 by a power of two.  A
+//    cycle of 8 x 1024 tokens, 16 experts of 1152 x 4608, takes 755 us with its down
+//    projections exact, 672 without.
 //
 //   up   : mid[r]  = q8(act(x[token(r)] . W_up[e]^T))   rows by the expert lists
 //   down : row of r = mid[r] . W_down[e]^T
@@ -1368,14 +1371,20 @@ hipError_t launch_up(const QArgs& a, bool exact, const FfnPlan& plan, hipStream_
                : launch_duo<kUp, ACT, float, false, 64>(a, st);
 }
 
+template <typename T, bool EXACT>
+hipError_t launch_down(const QArgs& a, const FfnPlan& plan, hipStream_t st) {
+  return plan.tm == 64 ? launch_duo<kDown, kActNone, T, EXACT, 64>(a, st)
+                       : launch_duo<kDown, kActNone, T, EXACT, 128>(a, st);
+}
+
 // Whether the 256 x 256 tiles can take a product: rows addressed by 32-bit byte
 // offsets, K long enough for the load stream's lookahead.
 bool tall_capable(int64_t rows, int K) {
   return q8_pitch(K) / kBlk >= kTallMinKT && rows * q8_pitch(K) < (int64_t(1) << 32);
 }
 
-// Whether the up projection takes the exact products (above).
-bool exact_up(const Shape& s) { return !s.bf16 || s.exact_hidden; }
+// Whether a layer's products are the exact ones (above).
+bool exact_products(const Shape& s) { return !s.bf16 || s.exact8; }
 
 // The tile height (32, 64, 128, or 256 for the 256-column tiles) that takes least
 // time: blocks come in rounds of two per CU, the last one perhaps of one, which is
@@ -1428,7 +1437,7 @@ Q8 q8_view(void* base, int64_t rows, int64_t K) {
 
 FfnPlan q8_plan(const Shape& s, int64_t rows) {
   FfnPlan p;
-  const bool exact = exact_up(s);
+  const bool exact = exact_products(s);
   // the rows of an expert vary: an eighth above the mean
   const int64_t mean = rows / s.E + rows / s.E / 8;
   auto tiles = [&](int n) {
@@ -1439,7 +1448,7 @@ FfnPlan q8_plan(const Shape& s, int64_t rows) {
   };
   const int ku = static_cast<int>(q8_pitch(s.d) / kBlk), kd = static_cast<int>(q8_pitch(s.d_ff) / kBlk);
   p.tm_up = q8_tile(tiles(s.up_rows()), ku, exact, !exact && tall_capable(s.tokens(), s.d), 64);
-  p.tm = q8_tile(tiles(s.d), kd, !s.bf16, s.bf16 && tall_capable(s.mid_rows(), s.d_ff), 64);
+  p.tm = q8_tile(tiles(s.d), kd, exact, !exact && tall_capable(s.mid_rows(), s.d_ff), 64);
   p.tall_up = p.tm_up == kTallTM;
   p.tall_down = p.tm == kTallTM;
   // Gated: 64-row tiles, one block per CU, where most experts have one.  Up, us, 64
@@ -1479,7 +1488,7 @@ hipError_t launch_q8_up(const Shape& s, int act, const FfnPlan& plan, const Quan
   a.qpitch = static_cast<int>(q8_pitch(s.d_ff));
   a.qspitch = static_cast<int>(q8_spitch(s.d_ff));
   a.tm = b.tiles + 2 * (s.groups() + 1);
-  const bool exact = exact_up(s);
+  const bool exact = exact_products(s);
   if (act == MOECA_ACT_SWIGLU) return launch_up<kActSwiglu>(a, exact, plan, st);
   if (act == MOECA_ACT_GELU_ERF) return launch_up<kActGeluErf>(a, exact, plan, st);
   return launch_up<kActGeluTanh>(a, exact, plan, st);
@@ -1510,11 +1519,9 @@ hipError_t launch_q8_down(const Shape& s, const FfnPlan& plan, const QuantWeight
   a.dst_sh = b.h_sh;
   a.tm = b.tiles + 2 * (s.groups() + 1) + 1;
   if (plan.tall_down) return launch_tall<kDown, kActNone, uint16_t>(a, st);
-  if (plan.tm == 64)
-    return s.bf16 ? launch_duo<kDown, kActNone, uint16_t, false, 64>(a, st)
-                  : launch_duo<kDown, kActNone, float, true, 64>(a, st);
-  return s.bf16 ? launch_duo<kDown, kActNone, uint16_t, false, 128>(a, st)
-                : launch_duo<kDown, kActNone, float, true, 128>(a, st);
+  if (!s.bf16) return launch_down<float, true>(a, plan, st);
+  return exact_products(s) ? launch_down<uint16_t, true>(a, plan, st)
+                           : launch_down<uint16_t, false>(a, plan, st);
 }
 
 int64_t q8_few_rows() { return 16; }

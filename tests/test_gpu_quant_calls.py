@@ -139,3 +139,43 @@ def test_noalloc_is_the_full_step(kw, cache):
     torch.cuda.synchronize()
     assert L.stats().full_step == 1
     assert torch.equal(y, z)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n,N", [(256, 1), (256, 60), (384, 700), (640, 4000)])
+def test_rows_of_an_8bit_cache_have_exact_products(n, N, dtype):
+    """Every eight consecutive products hold 448 * 448 and its negative besides small
+    integers, which instructions that align them to the largest and keep 2^-13 of it
+    would lose.  All sums are integers below 2^24, so fp32 has them exactly in any
+    order; large hidden values are their own GELU.  Output and cache are then known
+    to the bit: the integers, rounded once to the type."""
+    import torch
+    from paper_2606_15615_amd import _lib, quant
+    from paper_2606_15615_amd.layer import MoecaLayer
+    say(f"  {N} tokens of {n} {dtype}")
+    g = np.random.default_rng(n + N)
+    x = g.integers(8, 16, (N, n)) * 2.0                   # 16 .. 30: e4m3 numbers
+    x[:, ::8] = x[:, 4::8] = 448.0
+    down = g.integers(-2, 3, (2, n, n)).astype(float)
+    down[:, :, ::8], down[:, :, 4::8] = 448.0, -448.0
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    L = MoecaLayer(n, 2, 1, n, batch=1, tokens=N, dtype=dtype, experts="e4m3", cache="e4m3")
+    eye = torch.eye(n, device="cuda:0", dtype=t).expand(2, n, n).contiguous()
+    W_r = torch.from_numpy(g.normal(size=(2, n))).cuda().to(t)
+    L.set_weights_quant(W_r, None, quant.quantize_matrix(eye),
+                        quant.quantize_matrix(torch.from_numpy(down).cuda().to(t)))
+    L.reset()
+    xt = torch.from_numpy(x).cuda().to(t)[None]
+    y, z = torch.zeros_like(xt), torch.zeros_like(xt)
+    L.step(xt, 0, y)
+    _lib.moeca_forward_noalloc(L.h, xt.data_ptr(), 1, z.data_ptr(),
+                               torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    e = L.read("e_t")
+    h = np.einsum("nd,nkd->nk", x, down[e]) if N <= 60 else np.where(
+        (e == 0)[:, None], x @ down[0].T, x @ down[1].T)
+    assert np.abs(h).max() < 2 ** 15
+    h = torch.from_numpy(h).to(t)
+    assert torch.equal(y[0].cpu(), h) and torch.equal(z, y)
+    got = L.cache_rows().read(dtype=torch.float32).double().cpu().numpy()
+    np.testing.assert_array_equal(got, Q.round_trip(h.double().numpy()))
