@@ -394,13 +394,15 @@ int moeca_quant_matrix(const void* W, int dtype, int64_t count, int64_t N, int64
 /* out = x W^T (+ bias) for rows x [M][K] of the activation type, quantised by
  * the call, and a quantised matrix W of N rows: products of 8-bit operands with
  * both scales, fp32 sums, the bias (fp32 [N], or NULL) added in fp32, one
- * rounding to dtype.  For bf16 results the matrix instructions may align the
- * products of eight consecutive k to the largest of them and keep 2^-13 of it
- * (1.5e-5 of a row's 2-norm on normal values, where the rounding is 4e-3); fp32
- * results have exact products.  workspace: moeca_quant_linear_bytes(M, K) bytes, 256-byte
- * aligned, for the quantised rows; calls that overlap in time need one each.
- * M = 0 does nothing.  A row's sums do not depend on the other rows of the
- * call, except that M may choose another order of the sums over K. */
+ * rounding to dtype.  fp32 results, and bf16 results of at most 16 rows, have exact
+ * products: elements as bf16 times their scale (a scale under 2^-124 may lose
+ * elements under 2^-133).  For bf16 results of more rows the matrix instructions
+ * align the products of eight consecutive k to the largest of them and keep 2^-13
+ * of it (1.5e-5 of a row's 2-norm on normal values, where the rounding is 4e-3).
+ * workspace: moeca_quant_linear_bytes(M, K) bytes, 256-byte aligned, for the
+ * quantised rows; calls that overlap in time need one each.  M = 0 does nothing.
+ * A row's result does not depend on the values of the other rows; their number M
+ * may choose another order of the sums over K and, as above, the products. */
 size_t moeca_quant_linear_bytes(int64_t M, int64_t K);
 int moeca_quant_linear(const void* x, int dtype, int64_t M, int64_t K, int64_t ldx, const void* q,
                        const void* scale, int64_t N, const float* bias, void* out, int64_t ldo,

@@ -16,8 +16,9 @@
 // elements twenty times the others by 4e-5.  Next to a bf16 result's rounding
 // (4e-3) that is nothing, and they run at twice the bf16 rate.  Where it does
 // show, EXACT converts the operands in registers to bf16, which holds every
-// e4m3 number and power of two, and takes the bf16 instructions with fp32 sums:
-//  - fp32 results;
+// e4m3 number times a power of two down to 2^-133 (scales from 2^-124 on), and
+// takes the bf16 instructions with fp32 sums:
+//  - fp32 results, and those of at most 16 rows (a matter of latency, not of rate);
 //  - both products of a layer whose cache is 8-bit too, since what is cached is
 //    rounded to 8 bits once more.  Up: a hidden element that moves over a rounding
 //    border (1 in 200 does, at 1.5e-5) moves the down projection's row by 1.4e-3,

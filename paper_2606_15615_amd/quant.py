@@ -190,7 +190,9 @@ def linear_workspace(M, K, device="cuda:0"):
 
 def linear(x, W: QuantMatrix, bias=None, out=None, workspace=None, stream=None):
     """x W^T (+ bias) for rows x [M][K] (bfloat16 or float32; quantised by the call)
-    and one quantised matrix; ``out`` [M][N] is of x's type.  Without a
+    and one quantised matrix; ``out`` [M][N] is of x's type and overlaps no other
+    operand.  Products are exact for float32 results and for up to 16 rows; others
+    take the 8-bit matrix instructions (include/moeca.h states their precision).  Without a
     ``workspace`` one is allocated for the call, which then has to run on the
     current stream."""
     if W.q.ndim != 2:

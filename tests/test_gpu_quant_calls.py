@@ -179,3 +179,40 @@ def test_rows_of_an_8bit_cache_have_exact_products(n, N, dtype):
     assert torch.equal(y[0].cpu(), h) and torch.equal(z, y)
     got = L.cache_rows().read(dtype=torch.float32).double().cpu().numpy()
     np.testing.assert_array_equal(got, Q.round_trip(h.double().numpy()))
+
+
+U32 = 2.0 ** -24
+
+
+@pytest.mark.parametrize("M,dtype", [(6, "fp32"), (6, "bf16"), (16, "bf16"), (70, "fp32"),
+                                     (700, "fp32")])
+def test_exact_products_at_the_least_scale(M, dtype):
+    """Rows with the scale 2^-124 and every e4m3 number down to its subnormals, 2^-133
+    in all: the least elements of which products are exact.  All are wanted to within
+    the fp32 sums, K + 8 of half an ulp each of the magnitudes' sum, and one rounding."""
+    import torch
+    from paper_2606_15615_amd import quant
+    K, N = 640, 200
+    g = np.random.default_rng(M)
+    x = Q.TABLE[g.integers(0, 127, (M, K))]
+    x = np.where(g.random((M, K)) < 0.5, Q.TABLE[g.integers(0, 8, (M, K))], x)  # subnormals
+    x[:, ::128] = 448.0
+    x[0] = np.where(np.arange(K) % 128 == 0, 448.0, 2.0 ** -9)
+    x *= np.where(g.random((M, K)) < 0.5, -1.0, 1.0) * 2.0 ** -124
+    w = g.normal(size=(N, K)) / 2
+    w[:, ::128] = 0                     # the largest elements meet nothing
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    xt = torch.from_numpy(x).to(t).cuda()
+    np.testing.assert_array_equal(xt.double().cpu().numpy(), x)
+    wt = torch.from_numpy(w).cuda().to(torch.bfloat16)
+    q, s = Q.quant_rows(x)
+    assert (s == 3).all()
+    wv = Q.matrix_values(*Q.quant_matrix(wt.double().cpu().numpy()), K)
+    want, mag = x @ wv.T, np.abs(x) @ np.abs(wv).T
+    got = quant.linear(xt, quant.quantize_matrix(wt)).double().cpu().numpy()
+    half = 2.0 ** -8 if dtype == "bf16" else U32
+    # and half a step of the types' subnormals (2^-149, 2^-133)
+    least = 2.0 ** (-134 if dtype == "bf16" else -150)
+    tol = (K + 8) * (U32 * mag + 2.0 ** -150) + half * np.abs(want) + least
+    say(f"  {M} rows {dtype}: largest share of the bound {float((np.abs(got - want) / tol).max()):.3f}")
+    assert np.all(np.abs(got - want) <= tol)
