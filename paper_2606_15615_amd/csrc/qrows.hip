@@ -166,7 +166,7 @@ template <> struct Raw<uint16_t> {
   }
 };
 template <> struct Raw<float> {
-  typedef __attribute__((ext_vector_type(8))) unsigned int v;
+  typedef __attribute__((ext_vector_type(8), aligned(16))) unsigned int v;  // as rows are
   static __device__ __forceinline__ void widen(v x, float* f) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) f[u] = __uint_as_float(x[u]);

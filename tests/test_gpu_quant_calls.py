@@ -216,3 +216,45 @@ def test_exact_products_at_the_least_scale(M, dtype):
     tol = (K + 8) * (U32 * mag + 2.0 ** -150) + half * np.abs(want) + least
     say(f"  {M} rows {dtype}: largest share of the bound {float((np.abs(got - want) / tol).max()):.3f}")
     assert np.all(np.abs(got - want) <= tol)
+
+
+@pytest.mark.parametrize("k,d", [(2, 320), (2, 1152), (3, 192)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_buffers_at_odd_multiples_of_16_bytes(dtype, k, d):
+    """The C calls want 16-byte alignment and no more: attention features, input,
+    output and attention cache at 16 modulo 32."""
+    import torch
+    from paper_2606_15615_amd import quant
+    say(f"  {dtype} k {k} d {d}")
+    N = 45
+
+    def shifted(n, t):
+        size = torch.empty(0, dtype=t).element_size()
+        b = torch.zeros(n * size + 48, dtype=torch.uint8, device="cuda:0")
+        at = (16 - b.data_ptr()) % 32
+        b = b[at:at + n * size].view(t)
+        assert b.data_ptr() % 32 == 16
+        return b
+    L, x = _layer(d, 4, k, 128, 1, N, seed=d, dtype=dtype, experts="e4m3", cache="e4m3")
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(1)
+    a = torch.randn(N, d, generator=g, device="cuda:0").to(x.dtype)
+    got = []
+    for off in (False, True):
+        xs, ys, at = x, torch.zeros_like(x), a
+        rows = quant.QuantRows(N, d)
+        if off:
+            xs, ys, at = (shifted(N * d, x.dtype).view(1, N, d) for _ in range(3))
+            xs.copy_(x), at.copy_(a)
+            rows = quant.QuantRows(N, d, q=shifted(N * rows.pitch, torch.uint8).view(N, -1),
+                                   scale=shifted(N * rows.scale_pitch, torch.uint8).view(N, -1))
+        L.bind_attention(at, rows)
+        L.reset()
+        L.step(xs, 0, ys)
+        torch.cuda.synchronize()
+        got.append((ys.clone(), rows.q.clone(), rows.scale[:, :-(-d // 128)].clone(),
+                    rows.read()))
+    assert all(torch.equal(u, v) for u, v in zip(*got))
+    q, s = Q.quant_rows(a.double().cpu().numpy())
+    np.testing.assert_array_equal(got[1][1].cpu().numpy(), q)
+    np.testing.assert_array_equal(got[1][2].cpu().numpy(), s)
