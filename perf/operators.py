@@ -283,11 +283,24 @@ def prepare(case, seed):
     return s
 
 
+def _samples(c):
+    """Samples and tokens of each for a call of B N tokens.  A sample has at most 32768
+    branches where k is not 1, 2, 4 or 8; its tokens do not depend on each other here
+    (thresholds are above any score), so longer ones go in equal parts."""
+    B, N, k = c["B"], c["N"], c["k"]
+    if N * k > 32768 and 1024 % k:
+        most = 32768 // k
+        part = max(i for i in range(1, most + 1) if N % i == 0)
+        B, N = B * (N // part), part
+    return B, N
+
+
 def _make_layer(c, s):
     from paper_2606_15615_amd import _lib, quant
     from paper_2606_15615_amd.layer import MoecaLayer
     cached = c["kind"] == "cycle"
-    L = MoecaLayer(c["d"], c["E"], c["k"], c["d_ff"], batch=c["B"], tokens=c["N"],
+    B, N = _samples(c)
+    L = MoecaLayer(c["d"], c["E"], c["k"], c["d_ff"], batch=B, tokens=N,
                    mode=_lib.MOECA_MODE_THRESHOLD if cached else _lib.MOECA_MODE_FULL,
                    tau0=TAU0, alpha=ALPHA, act=c["act"], n_shared=c["n_shared"], device=DEV,
                    experts="e4m3" if c["eight"] else None, cache="e4m3" if cached else None)
