@@ -99,7 +99,10 @@ typedef struct moeca_layer moeca_layer;
  * hidden width d_ff (FFN_e(x) = W_down[e] act(W_up[e] x), Sec. 2.3).
  * Host only; the policy is copied.  Limits: 1 <= k <= min(E, 8), E <= 64,
  * 0 <= n_shared <= 8, d and d_ff multiples of 64, d <= 16384, d_ff <= 65536
- * (32768 with MOECA_ACT_SWIGLU), B*N*(k + n_shared) < 2^31.
+ * (32768 with MOECA_ACT_SWIGLU), B*N*(k + n_shared) < 2^31, and N*k <= 32768
+ * where k is not 1, 2, 4 or 8 (samples of more branches are decided in blocks of
+ * 1024, which have to end between tokens; an uncached layer's tokens can be
+ * given as more samples).
  * Returns NULL on a bad argument (moeca_last_error() says which). */
 moeca_layer* moeca_layer_create(int d, int E, int k, int d_ff, const moeca_policy* policy);
 
