@@ -212,6 +212,8 @@ def linear(x, W: QuantMatrix, bias=None, out=None, workspace=None, stream=None):
         raise ValueError(f"bias: expected a contiguous float32 vector of {W.N} on {device}")
     if M == 0:
         return out
+    if px == po:
+        raise ValueError("out is x: the product's blocks read x while others write out")
     if workspace is None:
         if stream is not None and stream != torch.cuda.current_stream(device):
             raise ValueError("a call on another stream needs a workspace of its own")

@@ -1,4 +1,4 @@
-"""On which stream the 8-bit wrappers allocate and launch: host checks, nothing runs
+"""What the 8-bit wrappers allocate, refuse and launch, and where: host checks, nothing runs
 on a GPU.  Launches and allocations are recorded in place of being made."""
 import pytest
 
@@ -80,3 +80,17 @@ def test_a_stream_of_another_device_is_refused():
         raise AssertionError("launched")
     with pytest.raises(ValueError, match="stream is one of cuda:1"):
         quant._launch(never, torch.device("cuda", 0), Stream(1))
+
+
+def test_a_product_in_place_is_refused(quant):
+    """Blocks of a product read rows of x while others write rows of out."""
+    import torch
+    W = quant.quantize_matrix(torch.empty(200, 200))
+    x = torch.empty(3, 200)
+    n = len(quant.launches)
+    with pytest.raises(ValueError, match="out is x"):
+        quant.linear(x, W, out=x)
+    assert len(quant.launches) == n
+    wide = torch.empty(3, 400)                     # halves of the same rows are apart
+    quant.linear(wide[:, :200], W, out=wide[:, 200:])
+    assert quant.linear(x[:0], W, out=x[:0]).shape == (0, 200)
