@@ -88,6 +88,7 @@ class MoecaLayer:
         self.h = handle
         self.workspace = workspace
         self._owned = False
+        self.up_rows = None  # of use with 8-bit experts alone, which blocks do not have
         self.experts8 = self.cache8 = False
         return self
 
@@ -104,7 +105,9 @@ class MoecaLayer:
 
     def _mats(self, ms, n, N, K):
         for m in ms:
-            if (m.q.ndim != 3 or m.q.shape[0] != n or (m.N, m.K) != (N, K) or
+            # (a layer whose experts are not in 8 bits is refused by the call itself)
+            if self.experts8 and (
+                    m.q.ndim != 3 or m.q.shape[0] != n or (m.N, m.K) != (N, K) or
                     m.q.device != self.device):
                 raise ValueError(f"expected {n} quantised matrices of {N} x {K} on {self.device}")
         return [t.data_ptr() for m in ms for t in (m.q, m.scale)]

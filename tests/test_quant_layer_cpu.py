@@ -62,3 +62,20 @@ def test_an_attention_cache_with_norms_is_refused(layer):
     with pytest.raises(ValueError, match="without a norm"):
         L.bind_attention(x, _rows(8, 128, norm=True))
     L.bind_attention(x, _rows(8, 128))
+
+
+def test_layers_with_plain_experts_refuse_8bit_weights(layer):
+    """A plain layer's, an 8-bit cache's and a stack's block alike."""
+    from paper_2606_15615_amd import _lib
+    from paper_2606_15615_amd.layer import MoecaLayer
+    p = _lib.moeca_policy_default()
+    p.batch, p.tokens = 1, 8
+    stack = _lib.moeca_stack_create(2, 128, 2, 4, 2, 64, p)
+    try:
+        block = MoecaLayer.attach(_lib.moeca_stack_layer(stack, 1), _bytes(16), 128, 4, 2, 64,
+                                  batch=1, tokens=8)
+        for L in (layer(n_shared=0), layer(cache="e4m3"), block):
+            with pytest.raises(_lib.MoecaError, match="not quantised"):
+                L.set_weights_quant(_bytes(4, 256), None, _stack(4, 64, 128), _stack(4, 128, 64))
+    finally:
+        _lib.moeca_stack_destroy(stack)
