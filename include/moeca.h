@@ -256,12 +256,14 @@ int moeca_cache_reset(moeca_layer* layer, void* stream);
 /* Tilings of the expert FFN's grouped GEMMs. */
 enum {
   MOECA_TILES_LARGE = 0,  /* 128 rows by 256 columns (bf16; fewer columns where
-                             the projection has fewer), or the fp32 tiles     */
+                             the projection has fewer), the fp32 tiles, or the
+                             8-bit ones of 64 or 128 rows                     */
   MOECA_TILES_STREAM = 1, /* 128 x 288, weight-streaming: few rows per expert;
                              a down projection adds K in four pieces          */
   MOECA_TILES_WIDE = 2,   /* all rows of an expert (384 at most) x 144: a few
                              hundred rows per expert; up projection only      */
-  MOECA_TILES_TALL = 3    /* 256 x 256: more rows                             */
+  MOECA_TILES_TALL = 3    /* 256 x 256: more rows (8-bit experts: 128 columns
+                             where few branches are recomputed)               */
 };
 typedef struct moeca_stats {
   int64_t n_branches;      /* B * N * k                                        */

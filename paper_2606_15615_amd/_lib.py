@@ -256,28 +256,8 @@ def moeca_quant_scale_pitch(K: int) -> int:
     return load().moeca_quant_scale_pitch(K)
 
 
-def moeca_quant_rows(src, dtype, rows, K, ld, slot, slots, q, scale, norm, stream) -> int:
-    return _check(load().moeca_quant_rows(src, dtype, rows, K, ld, slot, slots, q, scale, norm,
-                                          stream))
-
-
-def moeca_dequant_rows(q, scale, slots, K, slot, rows, dst, dtype, ld, stream) -> int:
-    return _check(load().moeca_dequant_rows(q, scale, slots, K, slot, rows, dst, dtype, ld,
-                                            stream))
-
-
-def moeca_quant_matrix(W, dtype, count, N, K, q, scale, stream) -> int:
-    return _check(load().moeca_quant_matrix(W, dtype, count, N, K, q, scale, stream))
-
-
 def moeca_quant_linear_bytes(M: int, K: int) -> int:
     return load().moeca_quant_linear_bytes(M, K)
-
-
-def moeca_quant_linear(x, dtype, M, K, ldx, q, scale, N, bias, out, ldo, workspace, nbytes,
-                       stream) -> int:
-    return _check(load().moeca_quant_linear(x, dtype, M, K, ldx, q, scale, N, bias, out, ldo,
-                                            workspace, nbytes, stream))
 
 
 # ---- block stack -----------------------------------------------------------

@@ -1405,13 +1405,13 @@ __global__ __launch_bounds__(kWideThreads, 1) void gemm_bf16_wide_kernel(
   }
 }
 
-// h_c[row_dst[r]] = bf16(((part[0][r] + part[1][r]) + ...) + part[S-1][r])
+// dst[row_dst[r]] = bf16(((part[0][r] + part[1][r]) + ...) + part[S-1][r])
 // for the listed rows r < off[E] (the down projection's K pieces, added in
 // piece order); one wave per row, 16 bytes of bf16 per lane and step.
 template <int SPLIT>
 __global__ __launch_bounds__(256) void reduce_partials_kernel(
     const float* __restrict__ part, int64_t part_rows, const int32_t* __restrict__ off,
-    const int32_t* __restrict__ row_dst, int E, int d, uint16_t* __restrict__ h_c) {
+    const int32_t* __restrict__ row_dst, int E, int d, uint16_t* __restrict__ dst) {
   const int lane = threadIdx.x & (kWave - 1);
   const int r = static_cast<int>(blockIdx.x) * 4 + static_cast<int>(threadIdx.x) / kWave;
   if (r >= off[E]) return;
@@ -1430,7 +1430,7 @@ __global__ __launch_bounds__(256) void reduce_partials_kernel(
         s1[u] = __fadd_rn(s1[u], a1[u]);
       }
     }
-    *reinterpret_cast<u32x4_t*>(h_c + drow * d + g * 8) =
+    *reinterpret_cast<u32x4_t*>(dst + drow * d + g * 8) =
         u32x4_t{pack2_bf16(s0[0], s0[1]), pack2_bf16(s0[2], s0[3]), pack2_bf16(s1[0], s1[1]),
                 pack2_bf16(s1[2], s1[3])};
   }
@@ -1789,11 +1789,11 @@ __global__ __launch_bounds__(kF32Threads, kF32Blocks) void gemm_f32_kernel(
   }
 }
 
-// h_c[row_dst[r]] = ((part[0][r] + part[1][r]) + ...) + part[split-1][r] for
+// dst[row_dst[r]] = ((part[0][r] + part[1][r]) + ...) + part[split-1][r] for
 // the listed rows r < off[E], one thread per four columns.
 __global__ __launch_bounds__(256) void reduce_partials_f32_kernel(
     const float* __restrict__ part, int64_t part_rows, const int32_t* __restrict__ off,
-    const int32_t* __restrict__ row_dst, int E, int d, int split, float* __restrict__ h_c) {
+    const int32_t* __restrict__ row_dst, int E, int d, int split, float* __restrict__ dst) {
   const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
   const int r = static_cast<int>(i / (d / 4)), g = static_cast<int>(i % (d / 4));
   if (r >= off[E]) return;
@@ -1805,7 +1805,7 @@ __global__ __launch_bounds__(256) void reduce_partials_f32_kernel(
 #pragma unroll
     for (int u = 0; u < 4; ++u) s[u] = __fadd_rn(s[u], v[u]);
   }
-  *reinterpret_cast<f32x4_t*>(h_c + int64_t(row_dst[r]) * d + g * 4) = s;
+  *reinterpret_cast<f32x4_t*>(dst + int64_t(row_dst[r]) * d + g * 4) = s;
 }
 
 constexpr int kBlocksPerCu = 2;

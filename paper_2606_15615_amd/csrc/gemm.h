@@ -61,7 +61,8 @@ __device__ __forceinline__ int tile_group(int L, int toff0, int toff1, int& firs
 // the A-operand source row and the output row (-1: padding, never stored;
 // padding rows re-read the tile's first row).  Routed groups (e < E): up
 // reads token list[r]/k and writes intermediate row r; down reads
-// intermediate row r and writes cache row row_dst[r].  Shared groups: up
+// intermediate row r and writes row row_dst[r] of the cache (of `fresh`, in list
+// order, where the cache is in 8 bits).  Shared groups: up
 // reads token r - off[e] and writes intermediate row r; down reads
 // intermediate row r and writes shared-output row r - off[E].
 template <int KIND>

@@ -101,7 +101,8 @@ struct Buffers {
   int32_t* tiles;   // [2][E+S+1] grouped-GEMM tile prefix per group (up, down), then the
                     // rows of a tile, at most, of either (256 x 256 tiles), then whether
                     // its columns are halved
-  int32_t* row_dst; // [B*N*k] cache row of each listed branch: (f/k)*k + sigma(f)
+  int32_t* row_dst; // [B*N*k] where each listed branch's row goes: cache row
+                    // (f/k)*k + sigma(f), or (cache8) its own place in the list
   int32_t* wide;    // [B][kWideWords] per-sample scratch of the multi-block decision path
   void* mid;        // [B*N*k + S*T][d_ff] FFN activation of listed and shared rows
   void* h_sh;       // [S][T][d] shared experts' outputs

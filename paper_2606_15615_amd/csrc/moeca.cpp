@@ -47,8 +47,8 @@ size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 enum Region {
   R_E_C, R_W_C, R_N_C, R_H_C, R_STAT, R_LOGITS, R_E_T, R_W_T, R_HBAR, R_TAU, R_MARGIN, R_Q,
   R_MASK, R_SIGMA, R_SYNC, R_OFF, R_LIST, R_POS, R_S_C,
-  R_FRESH, R_X8, R_CNT_BS, R_STATS_BS, R_RFLAGS, R_TILES, R_ROW_DST, R_ENT, R_CNT_CH, R_WIDE, R_MID, R_H_SH,
-  R_PART, R_COUNT
+  R_FRESH, R_X8, R_CNT_BS, R_STATS_BS, R_RFLAGS, R_TILES, R_ROW_DST, R_ENT, R_CNT_CH, R_WIDE,
+  R_MID, R_H_SH, R_PART, R_COUNT
 };
 
 struct Layout {
@@ -102,7 +102,7 @@ Layout make_layout(const Shape& s, bool external_mid = false, bool partials = tr
   b[R_WIDE] = size_t(s.B) * moeca::kWideWords * 4;
   b[R_MID] = external_mid ? 0 : mid_bytes(s);
   b[R_H_SH] = size_t(s.S) * ntok * s.d * act;
-  const int pieces = !partials || s.experts8    ? 1
+  const int pieces = !partials || s.experts8   ? 1
                      : moeca::thin_capable(s) ? moeca::kThinSplit
                                               : moeca::f32_split(s);
   b[R_PART] = pieces > 1 ? size_t(pieces) * size_t(s.mid_rows()) * s.d * 4 : 0;

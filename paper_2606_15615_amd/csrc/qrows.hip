@@ -28,7 +28,8 @@ constexpr int kMaxRowBlocks = 1 << 20;  // grid bound; rows beyond it by a strid
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kRowWaves * kWave) void quant_rows_kernel(
     const T* __restrict__ src, int64_t rows, int K, int64_t ld, const int32_t* __restrict__ slot,
-    const uint8_t* __restrict__ mask, int64_t slots, uint8_t* __restrict__ q, uint8_t* __restrict__ s, float* __restrict__ norm) {
+    const uint8_t* __restrict__ mask, int64_t slots, uint8_t* __restrict__ q,
+    uint8_t* __restrict__ s, float* __restrict__ norm) {
   const int lane = threadIdx.x & (kWave - 1);
   const int pitch = static_cast<int>(q8_pitch(K)), spitch = static_cast<int>(q8_spitch(K));
   for (int64_t r = int64_t(blockIdx.x) * kRowWaves + threadIdx.x / kWave; r < rows;
