@@ -600,11 +600,12 @@ __global__ __launch_bounds__(kMidThreads, 1) void qgemm_gated_kernel(QArgs a) {
 //
 // What bounds it: with many rows, EXACT, what a CU can load (20 bytes a clock; 16
 // experts of 1152 x 4608, 8 x 1024 tokens, up 206 us, 0.85 PFLOP/s of bf16
-// instructions); with few, the stream of the weights (256 tokens of the same layer: up
-// 85 MB in 21 to 25 us, 576 tiles for 512 places; down 20.5 us, 4.1 TB/s).  A ring of
-// six k-tiles instead of three left down at 21 and slowed up to 33 us (one block per
-// CU).  Four stages of half a k-tile, three ahead, in the LDS of the two stages of
-// 128 EXACT rows took 7 % longer.  Dense 333 x 1152 x 4608 10.9 us, 1000 rows 17.6 us.
+// instructions, down 167 us, 1.04); with few, the stream of the weights (256 tokens
+// of the same layer: up 85 MB in 21 to 25 us, 576 tiles for 512 places; down 20.5 us,
+// 4.1 TB/s).  A ring of six k-tiles instead of three left down at 21 and slowed up to
+// 33 us (one block per CU).  Four stages of half a k-tile, three ahead, in the LDS of
+// the two stages of 128 EXACT rows took 7 % longer.  Dense 333 x 1152 x 4608 10.9 us,
+// 1000 rows 17.6 us.
 // ---------------------------------------------------------------------------
 template <int TM, bool GATED> struct Duo {
   static constexpr int TN = GATED ? 256 : 128;
@@ -848,9 +849,10 @@ __global__ __launch_bounds__(256, (Duo<TM, ACT == kActSwiglu>::kBlocks)) void qg
 //
 // The rows of a tile, 256, 192 or 128, come from the lists kernel's table (dense:
 // from the host) as for the bf16 kernel, and so do its columns: 128 where tiles of
-// 256 would leave half of the CUs without one (a cache step that recomputes few
+// 256 would leave half of the CUs without one (a threshold step that recomputes few
 // branches, which the host cannot know); the second columns' region is not loaded
-// then (a cycle's down projections 49.1 -> 46.5 us on average).
+// then (16 experts of 1152 x 4608, 8 x 1024 tokens, down projections of a full step and
+// three such steps 49.1 -> 46.5 us on average).
 //
 // Measured: 16384 x 4608 x 4608 300 us, 2.3 PFLOP/s; 16 experts of 1152 x 4608, 8 x
 // 1024 tokens, up 180 us and down 98 us, 0.97 and 1.77 PFLOP/s; 64 gated experts of
@@ -1395,7 +1397,8 @@ bool exact_products(const Shape& s) { return !s.bf16 || s.exact8; }
 // the tile chosen is the fastest but for a few within 8 %.  Measured, us, 32 / 64 /
 // 128 rows / 256 columns: 129 x 1152 x 4608 9.7 11.0 13.4 19.6; 700 x 4608 x 4608
 // 44 33 37 48; 1500 x 1152 x 4608 25.3 22.2 19.5 23.9; 8192 x 4608 x 4608
-// 320 229 189 179.
+// 320 229 189 179.  (Gated up projections, which have tiles of their own, are weighed
+// against the 256-row tiles by the same figures.)
 // tiles(tm, tn): tiles of a height and width; least: the lowest height there is.
 template <typename F>
 int q8_tile(F tiles, int kt, bool exact, bool tall, int least) {

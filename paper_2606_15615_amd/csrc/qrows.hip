@@ -7,8 +7,9 @@
 // its largest magnitude four DPP steps; every element is loaded once and kept
 // in registers between the maximum and the conversion.  Measured, 16384 rows of
 // 1152, bf16: written with their norms in 12.9 us, 4.4 TB/s; read in 12.0 us, 4.7 TB/s
-// (a copy of 1 GiB: 5.2).  Asking for three groups of a row before using the first
-// took 0.8 us more.  154 rows take 4.2 us, a launch and two round trips.
+// (a copy of 1 GiB: 5.2), among other passes; under a kernel trace 14.2 and 13.0.
+// There, asking for three groups of a row before using the first took 0.8 us more
+// (14.3 -> 15.1).  154 rows take 4.2 us, a launch and two round trips.
 #include <algorithm>
 
 #include "common.h"

@@ -42,7 +42,7 @@ class MoecaLayer:
                  n_shared=0, device="cuda:0", experts=None, cache=None):
         """experts="e4m3": expert weights (and hidden rows) in 8 bits, bound with
         ``set_weights_quant``; cache="e4m3": the branch cache (and the attention
-        cache) in 8 bits."""
+        cache) in 8 bits.  With both, products are exact."""
         torch = _torch()
         if experts not in (None, "e4m3") or cache not in (None, "e4m3"):
             raise ValueError("experts and cache are None or 'e4m3'")
